@@ -58,7 +58,7 @@ typedef enum {
 } gelo_status;
 
 typedef enum { GELO_ORTHOGONAL = 0, GELO_NONORTHOGONAL = 1 } gelo_kind;
-typedef enum { GELO_F32 = 0, GELO_BF16 = 1, GELO_F16 = 2 } gelo_dtype;
+typedef enum { GELO_F32 = 0, GELO_BF16 = 1, GELO_F16 = 2, GELO_E4M3 = 3 /* elements of a paged cache only */ } gelo_dtype;
 
 /* Philox stream ids used by the library (third counter word). */
 enum { GELO_STREAM_G0 = 0, GELO_STREAM_G1 = 1, GELO_STREAM_SHIELD = 2, GELO_STREAM_POWER = 3 };
@@ -242,6 +242,11 @@ int gelo_quantize_e4m3(gelo_ctx* ctx, const void* X_dev, int rows, int cols, int
 int gelo_project_e4m3(gelo_ctx* ctx, const void* U8_dev, const float* u_scale_dev, const void* W8_dev, const float* w_scale_dev,
                       int m, int d, int p, void* Yp_dev, void* stream);
 
+/* The same with one scale per ROW of U: Yp_dev[i] = (u_scale_dev[i] * w_scale_dev[0]) * (U8[i] * W8), u_scale_dev m floats.
+ * Takes the rows that gelo_rms_norm left as codes. */
+int gelo_project_e4m3_rows(gelo_ctx* ctx, const void* U8_dev, const float* u_scale_dev, const void* W8_dev, const float* w_scale_dev,
+                           int m, int d, int p, void* Yp_dev, void* stream);
+
 /* Rows 0..n-1 of Ainv * Yp (shield rows are dropped by never computing them), split by
  * column thirds into Q_dev, K_dev, V_dev (each n x p/3; p % 3 == 0 and p/3 % 8 == 0).  If
  * K_dev and V_dev are both NULL the whole n x p result goes to Q_dev. */
@@ -350,6 +355,85 @@ int gelo_qkv_offload_blockdiag_batch(gelo_ctx* ctx, int calls, const void* const
                                      int n, int k, int d, int p, int block, const uint64_t* seeds,
                                      float shield_scale, int dtype, void* const* Q_dev, void* const* K_dev,
                                      void* const* V_dev, void* stream);
+
+/* ---- around the projection: norm, rotation, paged cache, attention of one new token -------------------------
+ *
+ * What a decoder layer does right before and right after the Q/K/V projection; the paper leaves these steps on the trusted side
+ * (Section 3.2 offloads the projection only).  Rows of X, R, Y, Q, K, V and O may lie further apart than their width: a row stride is given
+ * in elements and is a multiple of 8 (16 for codes).  Sums, norms and softmax statistics are held in fp32; every result is
+ * rounded once, to the type it is stored in.  The calls wait for nothing and can be captured into a graph. */
+
+/* Root-mean-square norm of `rows` rows of d values, with the residual's addition:
+ *     h = X + R (R_dev may be NULL: h = X),  y = h / sqrt(mean(h^2) + eps) * weight  (weight_dev, d values, may be NULL: 1).
+ *   R_out_dev (optional, only with R_dev; may be R_dev or X_dev itself) receives h.
+ *   Y_dev (optional; may be X_dev itself) receives y in `dtype`.
+ *   codes_dev (optional) receives E4M3 codes and row_scale_dev (rows floats) their scales: scale = max|y_row| / 448 (1 for a
+ *     row of zeros), code = nearest-even E4M3 of y / scale (y not rounded to `dtype` in between), saturating; with it d has to
+ *     be a multiple of 16.  A row that holds a NaN or an infinity gets a NaN scale and NaN codes.
+ * At least one of Y_dev and codes_dev is given.  y is formed from the unrounded h.  8 <= d <= 65536, a multiple of 8.  A row of magnitudes over
+ * 1e16 overflows the fp32 sum of squares and counts as infinite.  rows = 0 is a no-op. */
+int gelo_rms_norm(gelo_ctx* ctx, const void* X_dev, int ldx, const void* R_dev, int ldr, const void* weight_dev, int rows, int d,
+                  float eps, int dtype, void* R_out_dev, int ldro, void* Y_dev, int ldy, void* codes_dev, int ldc,
+                  float* row_scale_dev, void* stream);
+
+/* Rotary positions.  Pair i of the first `rot` components of a head turns by turns[i] of a full circle per position:
+ *     x_a' = (x_a cos - x_b sin) * magnitude,  x_b' = (x_b cos + x_a sin) * magnitude,   angle = 2 pi position turns[i],
+ * (a, b) = (i, i + rot / 2), or (2i, 2i + 1) if `interleaved`.  Components from `rot` on stay as they are.  The angle is reduced to one
+ * circle in binary64, so positions up to 2^31 - 1 keep fp32 accuracy.
+ * gelo_rope_turns fills turns_dev (rot / 2 doubles, 8-byte aligned) with t = base^(-2i / rot) / (2 pi), for long contexts stretched:
+ *     t' = t (g + (1 - g) / factor),  g = clamp((original * t - low) / (high - low), 0, 1),
+ * i.e. pairs that turn at least `high` times within the original context stay, those that turn at most `low` times are interpolated by
+ * `factor`, and a ramp lies between (Peng et al., "YaRN", 2023, Section 3.2).  original = 0 interpolates every pair by `factor` (1: plain). */
+typedef struct gelo_rope {
+    const double* turns_dev;       /* rot / 2 values */
+    int rot;                       /* even, 0 <= rot <= head_dim (0: nothing turns) */
+    int interleaved;
+    float magnitude;
+} gelo_rope;
+int gelo_rope_turns(gelo_ctx* ctx, int rot, double base, double factor, double original, double low, double high, double* turns_dev,
+                    void* stream);
+
+/* Y_dev = X_dev (n rows of heads x head_dim) rotated, row i to position pos_dev[i] (X_dev may be Y_dev with the same stride; rows whose
+ * position is negative are not written).  head_dim a multiple of 8, at most 256. */
+int gelo_rotary(gelo_ctx* ctx, const void* X_dev, int ldx, int n, int heads, int head_dim, const int* pos_dev, const gelo_rope* rope,
+                int dtype, void* Y_dev, int ldy, void* stream);
+
+/* A paged key-value cache: position t of sequence s lies in page table[s][t / page_size], at token t % page_size.  Element (page,
+ * token, head, component) is at page * page_stride + token * token_stride + head * head_stride + component, for keys and values
+ * alike, so pages may be laid out by token or by head.  Strides in elements, multiples of 16 bytes and at least head_dim; elements must not overlap.
+ * GELO_E4M3 stores codes of value / k_scale and value / v_scale (nearest-even, saturating); else both scales are 1.
+ * head_dim: a multiple of 8 (E4M3: of 16), at most 256.  The struct is host memory, read before a call returns. */
+typedef struct gelo_kv_cache {
+    void* k_dev;
+    void* v_dev;
+    const int* table_dev;          /* seqs x table_ld, the first max_pages columns are used */
+    long long page_stride, token_stride, head_stride;
+    int dtype;
+    int pages, page_size, kv_heads, head_dim;
+    int seqs, max_pages, table_ld;
+    float k_scale, v_scale;
+} gelo_kv_cache;
+
+/* Appends n tokens to a cache and rotates on the way: K_dev and V_dev (n rows of kv_heads x head_dim) go to position pos_dev[i] of sequence
+ * seq_dev[i] (NULL: token i belongs to sequence i), K rotated; Q_dev (n rows of q_heads x head_dim, may be NULL) rotated goes to Q_out_dev (may
+ * be Q_dev with the same stride).  rope NULL: nothing turns.  A token whose position is negative is left out: nothing of it is read or
+ * written (padding).  A sequence or position outside the table, or a page outside the cache, writes no key or value and records
+ * GELO_ERR_INVALID in the status word.  (sequence, position) pairs of one call have to differ.  The cache's type is `dtype`
+ * or, with a 16-bit dtype, GELO_E4M3. */
+int gelo_append_kv(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* K_dev, int ldk, const void* V_dev, int ldv, const void* Q_dev,
+                   int ldq, int q_heads, int n, const int* seq_dev, const int* pos_dev, const gelo_rope* rope, int dtype,
+                   void* Q_out_dev, int ldqo, void* stream);
+
+/* Attention of one new token per sequence: row s of Q_dev (cache->seqs rows of q_heads x head_dim; q_heads a multiple of kv_heads, head h
+ * reads key-value head h / (q_heads / kv_heads)) against positions max(0, len - window) .. len - 1 of sequence s, len = len_dev[s]
+ * (window 0: all):   o = sum_j p_j v_j,  p = softmax_j(scale q . k_j).   O_dev: rows as Q_dev (may be Q_dev itself with the same stride).
+ * lse_dev (optional, seqs x q_heads floats): log sum_j exp(scale q . k_j).  A length of zero or less gives o = 0 and lse = -infinity.
+ * Entries of the cache outside those positions are not read, or do not count whatever they hold.  A length beyond the table is cut to it, and a page
+ * outside the cache counts as absent; both record GELO_ERR_INVALID.  Rows of one call may share pages.  Needs a workspace
+ * of gelo_attention_workspace_bytes() bytes, whatever the sizes.  Results do not depend on what runs beside the call. */
+size_t gelo_attention_workspace_bytes(void);
+int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* Q_dev, int ldq, int q_heads, const int* len_dev,
+                         float scale, int window, int dtype, void* O_dev, int ldo, float* lse_dev, void* stream);
 
 /* ---- per-launch timing (measurement aid; no counterpart in the paper) ----------------------- */
 

@@ -19,16 +19,18 @@ _lib = None
 OK, ERR_INVALID, ERR_WORKSPACE, ERR_COND, ERR_TIMEOUT, ERR_CUDA, ERR_UNSUPPORTED = range(7)
 ORTHOGONAL, NONORTHOGONAL = 0, 1
 F32, BF16, F16 = 0, 1, 2
+E4M3 = 3                     # elements of a paged cache only
 STREAM_G0, STREAM_G1, STREAM_SHIELD, STREAM_POWER = 0, 1, 2, 3
 
 __all__ = [
     "OK", "ERR_INVALID", "ERR_WORKSPACE", "ERR_COND", "ERR_TIMEOUT", "ERR_CUDA", "ERR_UNSUPPORTED",
-    "ORTHOGONAL", "NONORTHOGONAL", "F32", "BF16", "F16", "GeloError", "Context", "load_library", "library_path",
+    "ORTHOGONAL", "NONORTHOGONAL", "F32", "BF16", "F16", "E4M3", "GeloError", "Context", "PagedCache", "Rope", "load_library", "library_path",
     "dtype_code", "EXPORTS",
 ]
 
 _vp, _i, _u32, _u64, _f, _sz = (ctypes.c_void_p, ctypes.c_int, ctypes.c_uint32, ctypes.c_uint64,
                                 ctypes.c_float, ctypes.c_size_t)
+_d = ctypes.c_double
 
 # name -> (restype, argtypes); mirrors include/gelo.h
 EXPORTS = {
@@ -58,6 +60,13 @@ EXPORTS = {
     "gelo_unmix": (_i, [_vp, _vp, _i, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
     "gelo_quantize_e4m3": (_i, [_vp, _vp, _i, _i, _i, _vp, _vp, _vp]),
     "gelo_project_e4m3": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp]),
+    "gelo_project_e4m3_rows": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp]),
+    "gelo_rms_norm": (_i, [_vp, _vp, _i, _vp, _i, _vp, _i, _i, _f, _i, _vp, _i, _vp, _i, _vp, _i, _vp, _vp]),
+    "gelo_rope_turns": (_i, [_vp, _i, _d, _d, _d, _d, _d, _vp, _vp]),
+    "gelo_rotary": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _i, _vp]),
+    "gelo_append_kv": (_i, [_vp, _vp, _vp, _i, _vp, _i, _vp, _i, _i, _i, _vp, _vp, _vp, _i, _vp, _i, _vp]),
+    "gelo_attention_workspace_bytes": (_sz, []),
+    "gelo_paged_attention": (_i, [_vp, _vp, _vp, _i, _i, _vp, _f, _i, _i, _vp, _i, _vp, _vp]),
     "gelo_qkv_offload": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _u64, _f, _i, _vp, _vp, _vp, _vp]),
     "gelo_project_unmix": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
     "gelo_set_small_batch_fusion": (_i, [_vp, _i]),
@@ -132,6 +141,62 @@ def _stream(stream):
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("turns_dev", _vp), ("rot", _i), ("interleaved", _i), ("magnitude", _f)]
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k_dev", _vp), ("v_dev", _vp), ("table_dev", _vp),
+                ("page_stride", ctypes.c_longlong), ("token_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
+                ("dtype", _i), ("pages", _i), ("page_size", _i), ("kv_heads", _i), ("head_dim", _i),
+                ("seqs", _i), ("max_pages", _i), ("table_ld", _i), ("k_scale", _f), ("v_scale", _f)]
+
+
+class Rope:
+    """A rotation: ``turns`` (float64, rot / 2 values, as ``Context.rope_turns`` fills it), the layout of a pair, a factor on the result.
+
+    Keeps the tensor alive; made once and handed to every call."""
+
+    def __init__(self, turns, interleaved=False, magnitude=1.0):
+        _want(turns, "turns", torch.float64, 1)
+        self.turns = turns if turns.is_contiguous() else turns.contiguous()
+        self.struct = _RopeStruct(self.turns.data_ptr(), 2 * turns.numel(), 1 if interleaved else 0, magnitude)
+        self.ref = ctypes.addressof(self.struct)
+
+
+class PagedCache:
+    """A paged key-value cache: ``k`` and ``v`` of shape (pages, page_size, kv_heads, head_dim) and ``table`` (sequences, pages per
+    sequence, int32).
+
+    Any strides do whose last one is 1 and which ``k`` and ``v`` share, so a cache laid out by head is passed transposed.  E4M3
+    caches are ``torch.float8_e4m3fn`` (or uint8) and have scales.  Keeps the tensors alive; made once and handed to every call."""
+
+    def __init__(self, k, v, table, k_scale=1.0, v_scale=1.0):
+        code = E4M3 if k.dtype in (torch.float8_e4m3fn, torch.uint8) else dtype_code(k.dtype)
+        _want(k, "k", k.dtype, 4)
+        _want(v, "v", k.dtype, 4)
+        _want(table, "table", torch.int32, 2)
+        if k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("k and v must have the same shape and strides, the last one 1")
+        if not k.device == v.device == table.device:
+            raise ValueError("k, v and table must be on one device")
+        if (table.shape[1] > 1 and table.stride(1) != 1) or (table.shape[0] > 1 and not table.shape[1] <= table.stride(0) < 1 << 31):
+            raise ValueError("the rows of table must be contiguous and apart")
+        self.k, self.v, self.table, self.dtype, self.device = k, v, table, code, k.device
+        self.pages, self.page_size, self.kv_heads, self.head_dim = k.shape
+        self.seqs = table.shape[0]
+        # the stride of a dimension of one entry is never used; torch reports any value for it
+        strides = [self.head_dim if k.shape[i] <= 1 else k.stride(i) for i in range(3)]
+        self.struct = _CacheStruct(k.data_ptr(), v.data_ptr(), table.data_ptr(), *strides, code, *k.shape, self.seqs, table.shape[1],
+                                   table.stride(0) if table.shape[0] > 1 else table.shape[1], k_scale, v_scale)
+        self.ref = ctypes.addressof(self.struct)
+
+
+def _want(t, name, dtype, dims):
+    if not t.is_cuda or t.dtype != dtype or t.dim() != dims:
+        raise ValueError(f"{name} must be a {dims}-dimensional CUDA tensor of {dtype}, not {t.dim()}-dimensional {t.dtype} on {t.device}")
 
 
 class Context:
@@ -299,6 +364,113 @@ class Context:
         """Yp (bf16) = u_scale * w_scale * (U8 @ W8) on E4M3 operands."""
         self._check(self._lib.gelo_project_e4m3(self._h, _ptr(U8), _ptr(u_scale), _ptr(W8), _ptr(w_scale), m, d, p, _ptr(Yp),
                                                 _stream(stream)), "gelo_project_e4m3")
+
+    def project_e4m3_rows(self, U8, u_scale, W8, w_scale, m, d, p, Yp, stream=None):
+        """Yp (bf16) = u_scale[:, None] * w_scale * (U8 @ W8) on E4M3 operands: a scale per row of U8 (as rms_norm leaves them)."""
+        self._check(self._lib.gelo_project_e4m3_rows(self._h, _ptr(U8), _ptr(u_scale), _ptr(W8), _ptr(w_scale), m, d, p, _ptr(Yp),
+                                                     _stream(stream)), "gelo_project_e4m3_rows")
+
+    # ---- around the projection -------------------------------------------------------------
+    def _rows(self, t, name, dtype, rows, width):
+        """Pointer and row stride of a matrix whose rows are contiguous."""
+        if t.device.index != self.device or not t.is_cuda:
+            raise ValueError(f"{name} is on {t.device}, the context on cuda:{self.device}")
+        if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+            raise ValueError(f"{name} must be {rows} x {width} of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+        if t.stride(1) != 1 and width > 1:
+            raise ValueError(f"the rows of {name} must be contiguous")
+        ld = t.stride(0) if rows > 1 else (width + 15) // 16 * 16      # (the stride of a single row is never used)
+        if ld >= 1 << 31:
+            raise ValueError(f"the rows of {name} are too far apart")
+        return t.data_ptr(), ld
+
+    def _vector(self, t, name, dtype, count):
+        if t.device.index != self.device or not t.is_cuda:
+            raise ValueError(f"{name} is on {t.device}, the context on cuda:{self.device}")
+        if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+            raise ValueError(f"{name} must hold {count} contiguous values of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+        return t.data_ptr()
+
+    def _on(self, stream):
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else _stream(stream)
+
+    def rms_norm(self, X, Y=None, weight=None, eps=1e-5, residual=None, residual_out=None, codes=None, row_scale=None, stream=None):
+        """Y = rms-normalised X + residual, times weight; residual_out = X + residual; codes and row_scale: the result in E4M3 (uint8 or
+        float8_e4m3fn) with a scale per row.  X: rows x d, rows may be strided; the type is X's."""
+        rows, d = X.shape
+        dt = X.dtype
+        x, ldx = self._rows(X, "X", dt, rows, d)
+        y, ldy = self._rows(Y, "Y", dt, rows, d) if Y is not None else (None, 0)
+        r, ldr = self._rows(residual, "residual", dt, rows, d) if residual is not None else (None, 0)
+        ro, ldro = self._rows(residual_out, "residual_out", dt, rows, d) if residual_out is not None else (None, 0)
+        c, ldc = (None, 0) if codes is None else self._rows(codes, "codes", codes.dtype if codes.element_size() == 1 else torch.uint8, rows, d)
+        s = self._vector(row_scale, "row_scale", torch.float32, rows) if row_scale is not None else None
+        w = self._vector(weight, "weight", dt, d) if weight is not None else None
+        self._check(self._lib.gelo_rms_norm(self._h, x, ldx, r, ldr, w, rows, d, eps, dtype_code(dt), ro, ldro, y, ldy, c, ldc, s,
+                                            self._on(stream)), "gelo_rms_norm")
+
+    def rope_turns(self, turns, base=10000.0, factor=1.0, original=0.0, low=1.0, high=32.0, stream=None):
+        """Fills turns (float64, rot / 2 values): turns per position of each pair, stretched for long contexts."""
+        t = self._vector(turns, "turns", torch.float64, turns.numel())
+        self._check(self._lib.gelo_rope_turns(self._h, 2 * turns.numel(), base, factor, original, low, high, t, self._on(stream)),
+                    "gelo_rope_turns")
+
+    def rotary(self, X, heads, pos, rope, Y=None, stream=None):
+        """Y (default: X itself) = X, n rows of `heads` heads, rotated to the positions pos (int32)."""
+        n, width = X.shape
+        Y = X if Y is None else Y
+        if heads < 1 or width % heads:
+            raise ValueError("the width of X must be a multiple of heads")
+        x, ldx = self._rows(X, "X", X.dtype, n, width)
+        y, ldy = self._rows(Y, "Y", X.dtype, n, width)
+        self._check(self._lib.gelo_rotary(self._h, x, ldx, n, heads, width // heads, self._vector(pos, "pos", torch.int32, n), rope.ref,
+                                          dtype_code(X.dtype), y, ldy, self._on(stream)), "gelo_rotary")
+
+    def append_kv(self, cache, K, V, pos, seq=None, rope=None, Q=None, Q_out=None, stream=None):
+        """K (rotated) and V, n rows of kv_heads heads, go to position pos[i] of sequence seq[i] (default i); Q rotated goes to Q_out
+        (default: Q itself)."""
+        n, width = K.shape[0], cache.kv_heads * cache.head_dim
+        dt = K.dtype
+        if cache.device.index != self.device:
+            raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
+        k, ldk = self._rows(K, "K", dt, n, width)
+        v, ldv = self._rows(V, "V", dt, n, width)
+        q, ldq, qo, ldqo, heads = None, 0, None, 0, 0
+        if Q is not None:
+            heads, rest = divmod(Q.shape[1], cache.head_dim)
+            if rest:
+                raise ValueError("the width of Q must be a multiple of head_dim")
+            q, ldq = self._rows(Q, "Q", dt, n, Q.shape[1])
+            qo, ldqo = (q, ldq) if Q_out is None else self._rows(Q_out, "Q_out", dt, n, Q.shape[1])
+        elif Q_out is not None:
+            raise ValueError("Q_out without Q")
+        s = self._vector(seq, "seq", torch.int32, n) if seq is not None else None
+        self._check(self._lib.gelo_append_kv(self._h, cache.ref, k, ldk, v, ldv, q, ldq, heads, n, s, self._vector(pos, "pos", torch.int32, n),
+                                             rope.ref if rope is not None else None, dtype_code(dt), qo, ldqo, self._on(stream)),
+                    "gelo_append_kv")
+
+    def ensure_attention_workspace(self):
+        """Allocates (with torch) a workspace large enough for paged_attention, if the current one is not."""
+        need = int(self._lib.gelo_attention_workspace_bytes())
+        if self._ws is None or self._ws.numel() * self._ws.element_size() < need:
+            self.set_workspace(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
+        return need
+
+    def paged_attention(self, cache, Q, lengths, O, scale=None, window=0, lse=None, stream=None):
+        """O = attention of one new token per sequence (row s of Q: q_heads heads) over the first lengths[s] positions of the cache, or the last
+        `window` of them; scale defaults to head_dim^-1/2; lse (sequences x q_heads, fp32) receives the logarithm of the softmax's sum."""
+        if cache.device.index != self.device:
+            raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
+        heads, rest = divmod(Q.shape[1], cache.head_dim)
+        if rest:
+            raise ValueError("the width of Q must be a multiple of head_dim")
+        dt = Q.dtype
+        q, ldq = self._rows(Q, "Q", dt, cache.seqs, Q.shape[1])
+        o, ldo = self._rows(O, "O", dt, cache.seqs, Q.shape[1])
+        ln = self._vector(lengths, "lengths", torch.int32, cache.seqs)
+        ls = self._vector(lse, "lse", torch.float32, cache.seqs * heads) if lse is not None else None
+        self._check(self._lib.gelo_paged_attention(self._h, cache.ref, q, ldq, heads, ln, cache.head_dim ** -0.5 if scale is None else scale,
+                                                   window, dtype_code(dt), o, ldo, ls, self._on(stream)), "gelo_paged_attention")
 
     def unmix(self, Ainv, lda, Yp, n, k, p, dtype, Q, K=None, V=None, stream=None):
         self._check(self._lib.gelo_unmix(self._h, _ptr(Ainv), lda, _ptr(Yp), n, k, p, dtype_code(dtype),

@@ -1,6 +1,9 @@
 // C-ABI entry points of the GELO offload library (see include/gelo.h): argument
 // validation, workspace carving and the launch sequences.  No entry point except
 // gelo_create / gelo_destroy allocates device memory.
+#include <limits.h>
+
+#include <cmath>
 #include <new>
 
 #include "common.cuh"
@@ -163,6 +166,35 @@ bool carve_ctx(gelo_ctx* ctx, int n, int k, int d, int p, int dtype, bool host_s
 bool bad_dtype(int t) { return t != GELO_F32 && t != GELO_BF16 && t != GELO_F16; }
 bool bad_ld(int lda, int m) { return lda < m || (lda % 8) != 0; }
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+constexpr int kMaxHeadDim = 256;
+
+// a row stride in elements for rows of `width`, in steps of `step`
+bool bad_row_stride(int ld, int width, int step) { return ld < width || (ld % step) != 0; }
+
+bool bad_rope(const gelo_rope& r, int head_dim)
+{
+    return r.rot < 0 || (r.rot % 2) != 0 || r.rot > head_dim ||
+           (r.rot > 0 && (!r.turns_dev || (reinterpret_cast<uintptr_t>(r.turns_dev) & 7u) || !std::isfinite(r.magnitude)));
+}
+
+// A paged cache that a call with activations of `dtype` can work on
+int check_cache(const gelo_kv_cache* c, int dtype)
+{
+    if (!c || !c->k_dev || !c->v_dev || misaligned(c->k_dev) || misaligned(c->v_dev) || c->pages < 1 || c->page_size < 1 ||
+        c->kv_heads < 1 || c->head_dim < 8 || (c->head_dim % 8) != 0 || c->head_dim > kMaxHeadDim || c->kv_heads > INT_MAX / c->head_dim ||
+        c->seqs < 0 || c->max_pages < 1 || c->table_ld < c->max_pages || (!c->table_dev && c->seqs > 0) || (reinterpret_cast<uintptr_t>(c->table_dev) & 3u))
+        return GELO_ERR_INVALID;
+    if (c->dtype != GELO_E4M3 && bad_dtype(c->dtype)) return GELO_ERR_INVALID;
+    if (!(c->k_scale > 0.0f) || !(c->v_scale > 0.0f) || !std::isfinite(c->k_scale) || !std::isfinite(c->v_scale)) return GELO_ERR_INVALID;
+    if (c->dtype != GELO_E4M3 && (c->k_scale != 1.0f || c->v_scale != 1.0f)) return GELO_ERR_INVALID;
+    const long long step = c->dtype == GELO_E4M3 ? 16 : 16 / (long long)elem_size(c->dtype);
+    if ((c->head_dim % step) != 0) return GELO_ERR_INVALID;
+    for (long long s : { c->page_stride, c->token_stride, c->head_stride })
+        if (s < c->head_dim || (s % step) != 0) return GELO_ERR_INVALID;
+    if (c->dtype == GELO_E4M3 ? dtype == GELO_F32 : c->dtype != dtype) return GELO_ERR_UNSUPPORTED;
+    return GELO_OK;
+}
 
 struct DeviceGuard {
     int prev = -1;
@@ -1178,7 +1210,17 @@ int gelo_project_e4m3(gelo_ctx* ctx, const void* U8_dev, const float* u_scale_de
         !w_scale_dev || !Yp_dev || misaligned(U8_dev) || misaligned(W8_dev) || misaligned(Yp_dev))
         return GELO_ERR_INVALID;
     DeviceGuard guard(ctx->device);
-    return launch_gemm_e4m3(ctx, m, p, d, U8_dev, d, W8_dev, p, u_scale_dev, w_scale_dev, Yp_dev, p, as_stream(stream));
+    return launch_gemm_e4m3(ctx, m, p, d, U8_dev, d, W8_dev, p, u_scale_dev, false, w_scale_dev, Yp_dev, p, as_stream(stream));
+}
+
+int gelo_project_e4m3_rows(gelo_ctx* ctx, const void* U8_dev, const float* u_scale_dev, const void* W8_dev, const float* w_scale_dev,
+                           int m, int d, int p, void* Yp_dev, void* stream)
+{
+    if (!ctx || m <= 0 || d <= 0 || p <= 0 || (d % 16) != 0 || (p % 16) != 0 || !U8_dev || !W8_dev || !u_scale_dev ||
+        !w_scale_dev || !Yp_dev || misaligned(U8_dev) || misaligned(W8_dev) || misaligned(Yp_dev))
+        return GELO_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    return launch_gemm_e4m3(ctx, m, p, d, U8_dev, d, W8_dev, p, u_scale_dev, true, w_scale_dev, Yp_dev, p, as_stream(stream));
 }
 
 int gelo_unmix(gelo_ctx* ctx, const void* Ainv_dev, int lda, const void* Yp_dev, int n, int k, int p, int dtype,
@@ -1339,6 +1381,90 @@ int gelo_qkv_offload_blockdiag_batch(gelo_ctx* ctx, int calls, const void* const
     DeviceGuard guard(ctx->device);
     return offload_blockdiag_impl(ctx, calls, H_dev, W_dev, n, k, d, p, block, seeds, shield_scale, dtype, Q_dev, K_dev,
                                   V_dev, as_stream(stream));
+}
+
+int gelo_rms_norm(gelo_ctx* ctx, const void* X_dev, int ldx, const void* R_dev, int ldr, const void* weight_dev, int rows, int d,
+                  float eps, int dtype, void* R_out_dev, int ldro, void* Y_dev, int ldy, void* codes_dev, int ldc,
+                  float* row_scale_dev, void* stream)
+{
+    if (!ctx || rows < 0 || d < 8 || (d % 8) != 0 || bad_dtype(dtype) || !(eps >= 0.0f)) return GELO_ERR_INVALID;
+    if (rows > 0 && ((!Y_dev && !codes_dev) || (codes_dev != nullptr) != (row_scale_dev != nullptr) || (R_out_dev && !R_dev))) return GELO_ERR_INVALID;
+    if (codes_dev && ((d % 16) != 0 || bad_row_stride(ldc, d, 16) || misaligned(codes_dev))) return GELO_ERR_INVALID;
+    if (d > 65536) return GELO_ERR_UNSUPPORTED;
+    if (rows == 0) return GELO_OK;
+    if (!X_dev || misaligned(X_dev) || misaligned(R_dev) || misaligned(weight_dev) || misaligned(R_out_dev) || misaligned(Y_dev) ||
+        (reinterpret_cast<uintptr_t>(row_scale_dev) & 3u) || bad_row_stride(ldx, d, 8) || (R_dev && bad_row_stride(ldr, d, 8)) ||
+        (R_out_dev && bad_row_stride(ldro, d, 8)) || (Y_dev && bad_row_stride(ldy, d, 8)))
+        return GELO_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    return launch_rms_norm(ctx, X_dev, ldx, R_dev, ldr, weight_dev, rows, d, eps, dtype, R_out_dev, ldro, Y_dev, ldy, codes_dev, ldc, row_scale_dev,
+                           as_stream(stream));
+}
+
+int gelo_rope_turns(gelo_ctx* ctx, int rot, double base, double factor, double original, double low, double high, double* turns_dev,
+                    void* stream)
+{
+    if (!ctx || rot < 0 || rot > kMaxHeadDim || (rot % 2) != 0 || !(base > 0.0) || !(factor > 0.0) || !(original >= 0.0) || !std::isfinite(base) ||
+        !std::isfinite(factor) || !std::isfinite(original) || (original > 0.0 && !(low < high)))
+        return GELO_ERR_INVALID;
+    if (rot == 0) return GELO_OK;
+    if (!turns_dev || (reinterpret_cast<uintptr_t>(turns_dev) & 7u)) return GELO_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    return launch_rope_turns(ctx, rot, base, factor, original, low, high, turns_dev, as_stream(stream));
+}
+
+int gelo_rotary(gelo_ctx* ctx, const void* X_dev, int ldx, int n, int heads, int head_dim, const int* pos_dev, const gelo_rope* rope,
+                int dtype, void* Y_dev, int ldy, void* stream)
+{
+    if (!ctx || n < 0 || heads < 1 || bad_dtype(dtype) || head_dim < 8 || (head_dim % 8) != 0 || head_dim > kMaxHeadDim || heads > INT_MAX / head_dim ||
+        bad_row_stride(ldx, heads * head_dim, 8) || bad_row_stride(ldy, heads * head_dim, 8) || !rope || bad_rope(*rope, head_dim))
+        return GELO_ERR_INVALID;
+    if (n == 0) return GELO_OK;
+    if (!X_dev || !Y_dev || !pos_dev || misaligned(X_dev) || misaligned(Y_dev) || (X_dev == Y_dev && ldx != ldy)) return GELO_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    return launch_rotate_append(ctx, nullptr, nullptr, 0, nullptr, 0, X_dev, ldx, heads, head_dim, n, nullptr, pos_dev, *rope, dtype, Y_dev, ldy,
+                                as_stream(stream));
+}
+
+int gelo_append_kv(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* K_dev, int ldk, const void* V_dev, int ldv, const void* Q_dev,
+                   int ldq, int q_heads, int n, const int* seq_dev, const int* pos_dev, const gelo_rope* rope, int dtype,
+                   void* Q_out_dev, int ldqo, void* stream)
+{
+    if (!ctx || n < 0 || bad_dtype(dtype) || (Q_dev != nullptr) != (Q_out_dev != nullptr)) return GELO_ERR_INVALID;
+    GELO_TRY(check_cache(cache, dtype));
+    const int dh = cache->head_dim, width = cache->kv_heads * dh;
+    const gelo_rope still = { nullptr, 0, 0, 1.0f };
+    if (!rope) rope = &still;
+    if (bad_rope(*rope, dh) || bad_row_stride(ldk, width, 8) || bad_row_stride(ldv, width, 8)) return GELO_ERR_INVALID;
+    if (Q_dev && (q_heads < 1 || q_heads > INT_MAX / dh || bad_row_stride(ldq, q_heads * dh, 8) || bad_row_stride(ldqo, q_heads * dh, 8) ||
+                  misaligned(Q_dev) || misaligned(Q_out_dev) || (Q_dev == Q_out_dev && ldq != ldqo)))
+        return GELO_ERR_INVALID;
+    if (n == 0) return GELO_OK;
+    if (!K_dev || !V_dev || !pos_dev || misaligned(K_dev) || misaligned(V_dev) || (!seq_dev && n > cache->seqs)) return GELO_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    return launch_rotate_append(ctx, cache, K_dev, ldk, V_dev, ldv, Q_dev, ldq, Q_dev ? q_heads : 0, dh, n, seq_dev, pos_dev, *rope, dtype, Q_out_dev, ldqo,
+                                as_stream(stream));
+}
+
+size_t gelo_attention_workspace_bytes(void) { return attend_workspace_bytes(); }
+
+int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* Q_dev, int ldq, int q_heads, const int* len_dev,
+                         float scale, int window, int dtype, void* O_dev, int ldo, float* lse_dev, void* stream)
+{
+    if (!ctx || bad_dtype(dtype) || window < 0 || !std::isfinite(scale)) return GELO_ERR_INVALID;
+    GELO_TRY(check_cache(cache, dtype));
+    const int dh = cache->head_dim;
+    if (q_heads < 1 || q_heads > INT_MAX / dh || (q_heads % cache->kv_heads) != 0 || bad_row_stride(ldq, q_heads * dh, 8) ||
+        bad_row_stride(ldo, q_heads * dh, 8))
+        return GELO_ERR_INVALID;
+    if (cache->seqs == 0) return GELO_OK;
+    if (!Q_dev || !O_dev || !len_dev || misaligned(Q_dev) || misaligned(O_dev) || (reinterpret_cast<uintptr_t>(lse_dev) & 3u) ||
+        (Q_dev == O_dev && ldq != ldo))
+        return GELO_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    if (!ctx->ws || ctx->ws_bytes < attend_workspace_bytes()) return GELO_ERR_WORKSPACE;
+    ctx->chain_valid = false;      // a later batch must not sample into the workspace before this call is done with it
+    return launch_paged_attention(ctx, *cache, Q_dev, ldq, q_heads, len_dev, scale, window, dtype, O_dev, ldo, lse_dev, ctx->ws, as_stream(stream));
 }
 
 int gelo_profile_start(gelo_ctx* ctx)

@@ -247,7 +247,7 @@ int launch_gemm_affine16(gelo_ctx*, int dtype, int M, int N, int K, const void* 
 int launch_quantize_e4m3(gelo_ctx*, const void* x, int rows, int cols, int ld, int dtype, void* out, int ldo, float* scale,
                          cudaStream_t);
 int launch_gemm_e4m3(gelo_ctx*, int M, int N, int K, const void* A8, int lda, const void* B8, int ldb, const float* sa,
-                     const float* sb, void* C, int ldc, cudaStream_t);
+                     bool sa_rows, const float* sb, void* C, int ldc, cudaStream_t);
 // The tensor core drops the 13 low mantissa bits of an fp32 operand instead of rounding them.  For values whose
 // mantissas are spread log-uniformly that loses 2^-11 / (2 ln 2) of the magnitude on average, coherently over all
 // terms of a product; a result whose operand was truncated is scaled back by 1 + kTf32TruncLoss per such operand,
@@ -269,6 +269,17 @@ struct Tf32x3Scratch {
     float* planes = nullptr;
     size_t c_elems = 0;
 };
+
+// ---- around the projection (norm.cu, rotary.cu, attend.cu); arguments as in gelo.h, checked by the entry points ----
+int launch_rms_norm(gelo_ctx*, const void* x, int ldx, const void* r, int ldr, const void* w, int rows, int d, float eps, int dtype,
+                    void* r_out, int ldro, void* y, int ldy, void* codes, int ldc, float* row_scale, cudaStream_t);
+int launch_rope_turns(gelo_ctx*, int rot, double base, double factor, double original, double low, double high, double* turns, cudaStream_t);
+// q and k / v may each be absent (null); kv is only read where k is given
+int launch_rotate_append(gelo_ctx*, const gelo_kv_cache* kv, const void* k, int ldk, const void* v, int ldv, const void* q, int ldq, int q_heads,
+                         int head_dim, int n, const int* seq, const int* pos, const gelo_rope& rope, int dtype, void* q_out, int ldqo, cudaStream_t);
+size_t attend_workspace_bytes();
+int launch_paged_attention(gelo_ctx*, const gelo_kv_cache& kv, const void* q, int ldq, int q_heads, const int* len, float scale, int window,
+                           int dtype, void* o, int ldo, float* lse, void* ws, cudaStream_t);
 
 // ---- projection and unmixing of a small batch in one kernel (decode.cu) ---------------------------------
 

@@ -6,37 +6,13 @@
 // order-free) and the cast, in which every thread works the scale out for itself.  Both are bound by reading x (16 bits: 2 bytes in,
 // 1 out per value); a thread keeps the loads of four rows in flight.  2150 x 4096 in bf16: 27 us with one row at a time, a launch for
 // the scale and one conversion instruction per value, 17 us.
-#include <cuda_fp8.h>
-
 #include "common.cuh"
+#include "vec8.cuh"
 
 namespace gelo {
 
 namespace {
 
-__device__ __forceinline__ float widen8(const __nv_bfloat16* e, int j) { return __bfloat162float(e[j]); }
-__device__ __forceinline__ float widen8(const __half* e, int j) { return __half2float(e[j]); }
-
-// Eight consecutive values of a row
-template <typename T>
-struct Eight {
-    uint4 raw[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* p)
-    {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = reinterpret_cast<const uint4*>(p)[i];
-    }
-    __device__ __forceinline__ void widen(float (&v)[8]) const
-    {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = reinterpret_cast<const float*>(raw)[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = widen8(reinterpret_cast<const T*>(raw), j);
-        }
-    }
-};
 constexpr int kQuantRows = 4;                                 // rows a thread has in flight
 
 template <typename T>
@@ -93,12 +69,9 @@ __global__ void __launch_bounds__(256) cast_e4m3_kernel(const T* __restrict__ x,
             const int row = r + u * (int)gridDim.y;
             float v[8];
             e[u].widen(v);
-            uint32_t c[2] = {0u, 0u};
 #pragma unroll
-            for (int j = 0; j < 8; j += 2)
-                c[j >> 2] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(__fdiv_rn(v[j], s), __fdiv_rn(v[j + 1], s)), __NV_SATFINITE, __NV_E4M3)
-                             << (8 * (j & 3));
-            if (row < rows) *reinterpret_cast<uint2*>(out + (size_t)row * ldo + 8 * g) = make_uint2(c[0], c[1]);
+            for (int j = 0; j < 8; ++j) v[j] = __fdiv_rn(v[j], s);
+            if (row < rows) *reinterpret_cast<uint2*>(out + (size_t)row * ldo + 8 * g) = e4m3_codes(v);
         }
     }
 }

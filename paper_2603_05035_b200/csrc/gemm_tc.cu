@@ -69,8 +69,9 @@ struct TcParams {
     float post_scale;               //   ... and the factor applied after that: out = post_scale * (out_scale * acc - diag_sub [row == col])
     int a3d, b3d;                   // the MN-major A tile / the B tile arrives as ONE three-dimensional box (see make_map_nmajor)
     int out_f16;                    // TC_STORE_BF16: operands and output are IEEE half instead of bfloat16
-    const float* scale_a;           // TC_STORE_BF16 with 8-bit operands: the per-tensor scales (device scalars); the
+    const float* scale_a;           // TC_STORE_BF16 with 8-bit operands: the scales of the operands (device memory, B's a scalar); the
     const float* scale_b;           //   accumulator is multiplied by their product before it is rounded
+    int scale_a_step;               //   0: A's scale is a scalar, 1: one per row
     const void* add; int ldadd;     // TC_AFFINE16: out = out_scale * acc + diag_sub on the diagonal + post_scale * the entry of `add` (optional)
     int tri, tri_tiles;             // TC_STORE_SYM16: the result is symmetric; only the tri_tiles tiles that reach the diagonal or lie
                                     // above it are computed, and what lies below them is filled in by mirroring
@@ -199,7 +200,7 @@ __device__ __forceinline__ void store_tile16(const TcParams& prm, uint32_t taddr
 {
     const bool affine = prm.mode == TC_AFFINE16;
     const int gm = m0 + lane;
-    const float sc = affine ? prm.out_scale : (prm.scale_a ? prm.scale_a[0] * prm.scale_b[0] : 1.0f);
+    const float sc = affine ? prm.out_scale : (prm.scale_a ? prm.scale_a[prm.scale_a_step * min(gm, prm.M - 1)] * prm.scale_b[0] : 1.0f);
     if (affine && prm.add) {
         const int n = gn + 8 * (lane & 7);
 #pragma unroll
@@ -1468,10 +1469,10 @@ int launch_gemm_affine16(gelo_ctx* ctx, int dtype, int M, int N, int K, const vo
 }
 
 // Y (M x N, bf16) = (sa sb) A8 (M x K, E4M3, row stride lda bytes) * B8 (K x N, E4M3, row stride ldb bytes): the offloaded
-// product on 8-bit operands (kind::f8f6f4, fp32 accumulation), sa and sb device scalars.  A stage holds 128 bytes of
+// product on 8-bit operands (kind::f8f6f4, fp32 accumulation), sb a device scalar, sa one too or (sa_rows) one per row.  A stage holds 128 bytes of
 // k per A row, i.e. 128 values, and the matching 128 rows of B in boxes of 128 columns.
 int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda, const void* B8, int ldb, const float* sa,
-                     const float* sb, void* C, int ldc, cudaStream_t st)
+                     bool sa_rows, const float* sb, void* C, int ldc, cudaStream_t st)
 {
     if (M <= 0 || N <= 0 || K <= 0) return GELO_OK;
     if (!ctx->tmap_encode) return GELO_ERR_CUDA;
@@ -1501,6 +1502,7 @@ int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda
     p.C0 = C; p.C1 = C; p.C2 = C;
     p.ldc = ldc; p.csplit = N;
     p.scale_a = sa; p.scale_b = sb;
+    p.scale_a_step = sa_rows ? 1 : 0;
     p.status = ctx->status_dev;
     return launch_tiles<256, false, false, false, true>(ctx, pair, ma, ma, mb, mb, ma, p, 2.0 * M * (double)N * K, st);
 }

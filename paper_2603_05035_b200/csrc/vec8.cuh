@@ -1,0 +1,55 @@
+// Eight consecutive values of a row in registers: 16-byte loads and stores, widening to fp32 and rounding back.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <stdint.h>
+
+namespace gelo {
+
+__device__ __forceinline__ float widen_at(const __nv_bfloat16* e, int j) { return __bfloat162float(e[j]); }
+__device__ __forceinline__ float widen_at(const __half* e, int j) { return __half2float(e[j]); }
+__device__ __forceinline__ float widen_at(const float* e, int j) { return e[j]; }
+__device__ __forceinline__ float widen_at(const uint8_t* e, int j) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(e[j], __NV_E4M3))); }
+
+__device__ __forceinline__ void round_to(float v, float* out) { *out = v; }
+__device__ __forceinline__ void round_to(float v, __nv_bfloat16* out) { *out = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void round_to(float v, __half* out) { *out = __float2half_rn(v); }
+
+template <typename T>
+struct Eight {
+    uint4 raw[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = raw[i];
+    }
+    __device__ __forceinline__ void widen(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = widen_at(reinterpret_cast<const T*>(raw), j);
+    }
+    __device__ __forceinline__ void narrow(const float (&v)[8])
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) round_to(v[j], reinterpret_cast<T*>(raw) + j);
+    }
+};
+
+// Eight E4M3 codes, nearest-even, saturating at +-448; a NaN stays one
+__device__ __forceinline__ uint2 e4m3_codes(const float (&v)[8])
+{
+    uint32_t c[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; j += 2)
+        c[j >> 2] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[j], v[j + 1]), __NV_SATFINITE, __NV_E4M3) << (8 * (j & 3));
+    return make_uint2(c[0], c[1]);
+}
+
+}  // namespace gelo
