@@ -68,8 +68,8 @@ typedef struct gelo_ctx gelo_ctx;
 /* ---- context ------------------------------------------------------------------- */
 
 /* Creates a context on CUDA device `device` (must be compute capability 10.x, else
- * GELO_ERR_UNSUPPORTED).  Allocates a few hundred bytes of device and pinned host
- * memory for the status word.  *ctx is NULL on failure. */
+ * GELO_ERR_UNSUPPORTED).  Allocates a few KB of device and pinned host
+ * memory for the status word and for counters.  *ctx is NULL on failure. */
 int gelo_create(gelo_ctx** ctx, int device);
 int gelo_destroy(gelo_ctx* ctx);
 

@@ -911,8 +911,11 @@ int gelo_create(gelo_ctx** out, int device)
     ctx->sm_count = prop.multiProcessorCount;
     if (cudaMalloc(&ctx->status_dev, kStatusWords * sizeof(int)) != cudaSuccess ||
         cudaMemset(ctx->status_dev, 0, kStatusWords * sizeof(int)) != cudaSuccess ||
+        cudaMalloc(&ctx->attend_arrived, attend_counter_bytes()) != cudaSuccess ||
+        cudaMemset(ctx->attend_arrived, 0, attend_counter_bytes()) != cudaSuccess ||
         cudaHostAlloc(&ctx->status_host, kStatusWords * sizeof(int), cudaHostAllocDefault) != cudaSuccess) {
         if (ctx->status_dev) cudaFree(ctx->status_dev);
+        if (ctx->attend_arrived) cudaFree(ctx->attend_arrived);
         delete ctx;
         return GELO_ERR_CUDA;
     }
@@ -972,6 +975,7 @@ int gelo_destroy(gelo_ctx* ctx)
     if (ctx->lane_seed_dev) cudaFree(ctx->lane_seed_dev);
     if (ctx->batch_start) cudaEventDestroy(ctx->batch_start);
     cudaFree(ctx->status_dev);
+    cudaFree(ctx->attend_arrived);
     cudaFreeHost(ctx->status_host);
     delete ctx;
     return GELO_OK;

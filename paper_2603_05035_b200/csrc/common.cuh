@@ -53,6 +53,7 @@ struct gelo_ctx {
     size_t ws_bytes = 0;
     int* status_dev = nullptr;
     int* status_host = nullptr;   // pinned mirror
+    int* attend_arrived = nullptr;   // counters of the attention's CTAs, zero between calls (attend.cu)
     float gamma = 0.5f;
     float cond_bound = 100.0f;
     int max_attempts = 8;
@@ -278,6 +279,7 @@ int launch_rope_turns(gelo_ctx*, int rot, double base, double factor, double ori
 int launch_rotate_append(gelo_ctx*, const gelo_kv_cache* kv, const void* k, int ldk, const void* v, int ldv, const void* q, int ldq, int q_heads,
                          int head_dim, int n, const int* seq, const int* pos, const gelo_rope& rope, int dtype, void* q_out, int ldqo, cudaStream_t);
 size_t attend_workspace_bytes();
+size_t attend_counter_bytes();
 int launch_paged_attention(gelo_ctx*, const gelo_kv_cache& kv, const void* q, int ldq, int q_heads, const int* len, float scale, int window,
                            int dtype, void* o, int ldo, float* lse, void* ws, cudaStream_t);
 
