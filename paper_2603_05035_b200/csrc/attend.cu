@@ -3,7 +3,7 @@
 // One pass over the keys and values with the running maximum and sum of the softmax; every key and value is read once for all query
 // heads that share it (up to 16; more heads read them again, from L2).  Bound by HBM: 4 heads-per-group flops per element read.
 //
-// The work of a call is one line of tiles: sequence after sequence, key-value head after head, 16 positions a tile.  Every CTA works out
+// The work of a call is one line of tiles: sequence after sequence, key-value head after head, 16 or 32 positions a tile.  Every CTA works out
 // from the lengths which equal share of that line is its own, so ragged lengths balance and one long sequence fills the GPU.  What of
 // a (sequence, head) falls to one CTA is a segment; where a CTA's border cuts one, each side leaves its sums in the workspace and the
 // CTA that arrives last adds them up, in the order of the CTAs whoever that is.
@@ -20,7 +20,6 @@ namespace gelo {
 
 namespace {
 
-constexpr int kTile = 16;                                     // positions of a tile
 constexpr int kMaxCtas = 320;
 constexpr int kMaxParts = 64;                                 // a head's sums come from no more than about so many CTAs
 constexpr int kSlotFloats = 16 * 256 + 32;                    // sums of 16 heads, their maxima, their totals
@@ -43,11 +42,12 @@ struct AttendArgs {
 
 // The positions that count of one sequence, and its tiles
 struct Span { int first, len, t0, t1; };
+template <int kTile>
 __device__ __forceinline__ Span span_of(const AttendArgs& p, int seq)
 {
     Span s;
     const long long room = (long long)p.max_pages * p.page_size;
-    const int cap = room < INT_MAX - kTile ? (int)room : INT_MAX - kTile;
+    const int cap = room < INT_MAX - kTile ? (int)room : INT_MAX - kTile;             // (a tile's last position is still an int)
     int n = p.len[seq];
     if (n > cap) {
         n = cap;
@@ -61,6 +61,7 @@ __device__ __forceinline__ Span span_of(const AttendArgs& p, int seq)
 }
 
 // A walk over the segments of a CTA's share
+template <int kTile>
 struct Walk {
     Span s;
     int seq, unit, at, end;                                   // the segment: tiles [at, end) of (seq, unit)
@@ -68,7 +69,7 @@ struct Walk {
     __device__ __forceinline__ void begin(const AttendArgs& p, int seq0, long long offset, long long tiles)
     {
         seq = seq0;
-        s = span_of(p, seq);
+        s = span_of<kTile>(p, seq);
         const int n = s.t1 - s.t0;
         unit = (int)(offset / n);
         at = s.t0 + (int)(offset - (long long)unit * n);
@@ -80,7 +81,7 @@ struct Walk {
         if (left <= 0) return false;
         if (++unit == p.units) {
             unit = 0;
-            s = span_of(p, ++seq);
+            s = span_of<kTile>(p, ++seq);
         }
         at = s.t0;
         end = at + (int)min((long long)(s.t1 - at), left);
@@ -90,7 +91,7 @@ struct Walk {
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there)      // zeros where nothing is there
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there)      // zeros where nothing is there; `src` is not read then
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
@@ -121,6 +122,13 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 2^x for x <= 0, to two units in the last place; nothing where the result is no normal number
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 template <typename M>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 {
@@ -137,17 +145,19 @@ __device__ __forceinline__ float rest(float x)
     round_to(x, &e);
     return x - widen_at(&e, 0);
 }
-__device__ __forceinline__ uint32_t half2_of_codes(uint32_t two)                       // the low 16 bits: two E4M3 codes
+// four E4M3 codes as halves: the low two, the high two
+__device__ __forceinline__ void halves_of_codes(uint32_t four, uint32_t& low, uint32_t& high)
 {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(low), "=r"(high) : "r"(four));
 }
 
-// Geometry of a kernel instance.  Rows of DH elements of kBytes; the 16-byte pieces of a row are permuted by its number so that eight
+// Geometry of a kernel instance.  Rows of DH elements of kBytes, 32 of them where that is no more than 8 KB of keys and values, since what a tile
+// costs beside its products is the same; the 16-byte pieces of a row are permuted by its number so that eight
 // rows' pieces of one column lie in different banks.
 template <int DH, int kBytes>
 struct Tiles {
     static constexpr int kRow = DH * kBytes;                  // bytes
+    static constexpr int kTile = kRow <= 128 ? 32 : 16;       // positions
     static constexpr int kPieces = kRow / 16;                 // of a row
     static constexpr int kHalf = kTile * kRow;                // the keys, or the values
     static constexpr int kStage = 2 * kHalf;
@@ -234,64 +244,81 @@ struct MmaWarp {
 
     __device__ __forceinline__ void tile(uint32_t keys, uint32_t values, uint32_t counts, int lane)
     {
+        constexpr int kSub = G::kTile / 16;
         const int r = lane >> 2;
-        float c[NT][4];
+        float c[kSub][NT][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int b = 0; b < kSub; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) c[n][j] = 0.0f;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[b][n][j] = 0.0f;
         // matrix i of a load comes from the addresses of lanes 8i .. 8i + 7: rows 0-7 and 8-15, then the next piece of both
         const int row = lane & 15, next = lane >> 4;
-        if constexpr (kCodes) {
 #pragma unroll
-            for (int s = 0; s < DH / 16; s += 2) {
-                uint32_t x[4];
-                ldmatrix4(x, keys + G::piece(row, s + next));
+        for (int b = 0; b < kSub; ++b) {
+            if constexpr (kCodes) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t a[4] = {half2_of_codes(x[2 * u] & 0xffffu), half2_of_codes(x[2 * u + 1] & 0xffffu), half2_of_codes(x[2 * u] >> 16),
-                                           half2_of_codes(x[2 * u + 1] >> 16)};
+                for (int s = 0; s < DH / 16; s += 2) {
+                    uint32_t x[4];
+                    ldmatrix4(x, keys + G::piece(16 * b + row, s + next));
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma(c[n], a, qf[s + u][n][0], qf[s + u][n][1], M());
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t a[4];
+                        halves_of_codes(x[2 * u], a[0], a[2]);
+                        halves_of_codes(x[2 * u + 1], a[1], a[3]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma(c[b][n], a, qf[s + u][n][0], qf[s + u][n][1], M());
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < DH / 16; ++s) {
+                    uint32_t a[4];
+                    ldmatrix4(a, keys + G::piece(16 * b + row, 2 * s + next));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma(c[b][n], a, qf[s][n][0], qf[s][n][1], M());
                 }
             }
-        } else {
-#pragma unroll
-            for (int s = 0; s < DH / 16; ++s) {
-                uint32_t a[4];
-                ldmatrix4(a, keys + G::piece(row, 2 * s + next));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma(c[n], a, qf[s][n][0], qf[s][n][1], M());
-            }
         }
-        const bool on0 = (counts >> r) & 1u, on1 = (counts >> (r + 8)) & 1u;
-        uint32_t ph[NT][2], pl[NT][2];
+        // positions of this lane: r + 8 i
+        bool on[2 * kSub];
+#pragma unroll
+        for (int i = 0; i < 2 * kSub; ++i) on[i] = (counts >> (r + 8 * i)) & 1u;
+        uint32_t ph[kSub][NT][2], pl[kSub][NT][2];
         bool moved = false;
         float keep[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float e[4];
+            float e[2 * kSub][2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float s0 = on0 ? c[n][j] * scale[n][j] : kNone, s1 = on1 ? c[n][2 + j] * scale[n][j] : kNone;
-                float top = fmaxf(s0, s1);
+                float top = kNone;
+#pragma unroll
+                for (int i = 0; i < 2 * kSub; ++i) {
+                    e[i][j] = on[i] ? c[i >> 1][n][2 * (i & 1) + j] * scale[n][j] : kNone;
+                    top = fmaxf(top, e[i][j]);
+                }
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
                 top = fmaxf(top, m[n][j]);
                 const float base = top == kNone ? 0.0f : top;
-                keep[n][j] = exp2f(m[n][j] - base);
+                keep[n][j] = power2(m[n][j] - base);
                 moved |= top > m[n][j];
                 m[n][j] = top;
-                e[j] = on0 ? exp2f(s0 - base) : 0.0f;
-                e[2 + j] = on1 ? exp2f(s1 - base) : 0.0f;
-                l[n][j] = l[n][j] * keep[n][j] + (e[j] + e[2 + j]);
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 2 * kSub; ++i) {
+                    e[i][j] = power2(e[i][j] - base);         // (nothing for minus infinity)
+                    sum += e[i][j];
+                }
+                l[n][j] = fmaf(l[n][j], keep[n][j], sum);
             }
-            ph[n][0] = transposed(pack2<M>(e[0], e[1]));
-            ph[n][1] = transposed(pack2<M>(e[2], e[3]));
-            if constexpr (kPair) {
-                pl[n][0] = transposed(pack2<M>(rest<M>(e[0]), rest<M>(e[1])));
-                pl[n][1] = transposed(pack2<M>(rest<M>(e[2]), rest<M>(e[3])));
+#pragma unroll
+            for (int i = 0; i < 2 * kSub; ++i) {
+                ph[i >> 1][n][i & 1] = transposed(pack2<M>(e[i][0], e[i][1]));
+                if constexpr (kPair) pl[i >> 1][n][i & 1] = transposed(pack2<M>(rest<M>(e[i][0]), rest<M>(e[i][1])));
             }
         }
         if (__any_sync(0xffffffffu, moved)) {
@@ -302,34 +329,36 @@ struct MmaWarp {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[s][n][j] *= keep[n][j & 1];
         }
-        if constexpr (kCodes) {
-            // an 8 x 8 transposed load hands out code pairs: components 2r and 2r + 1 of two positions; the first become row r, the second row r + 8
-            const int pos = (lane & 7) + ((lane >> 4) << 3), col = (lane >> 3) & 1;
+        const int pos = (lane & 7) + ((lane >> 4) << 3), col = (lane >> 3) & 1;
 #pragma unroll
-            for (int s = 0; s < DH / 16; s += 2) {
-                uint32_t x[4];
-                ldmatrix4_t(x, values + G::piece(pos, s + col));
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t near = __byte_perm(x[u], 0, 0x3120), far = __byte_perm(x[2 + u], 0, 0x3120);
-                    const uint32_t a[4] = {half2_of_codes(near & 0xffffu), half2_of_codes(near >> 16), half2_of_codes(far & 0xffffu), half2_of_codes(far >> 16)};
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma(acc[s + u][n], a, ph[n][0], ph[n][1], M());
-                        if constexpr (kPair) mma(acc[s + u][n], a, pl[n][0], pl[n][1], M());
-                    }
-                }
-            }
-        } else {
-            const int pos = (lane & 7) + ((lane >> 4) << 3), col = (lane >> 3) & 1;
-#pragma unroll
-            for (int s = 0; s < DH / 16; ++s) {
-                uint32_t a[4];
-                ldmatrix4_t(a, values + G::piece(pos, 2 * s + col));
+        for (int b = 0; b < kSub; ++b) {
+            auto add = [&](int s, const uint32_t (&a)[4]) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    mma(acc[s][n], a, ph[n][0], ph[n][1], M());
-                    if constexpr (kPair) mma(acc[s][n], a, pl[n][0], pl[n][1], M());
+                    mma(acc[s][n], a, ph[b][n][0], ph[b][n][1], M());
+                    if constexpr (kPair) mma(acc[s][n], a, pl[b][n][0], pl[b][n][1], M());
+                }
+            };
+            if constexpr (kCodes) {
+                // an 8 x 8 transposed load hands out code pairs: components 2r and 2r + 1 of two positions; the first become row r, the second row r + 8
+#pragma unroll
+                for (int s = 0; s < DH / 16; s += 2) {
+                    uint32_t x[4];
+                    ldmatrix4_t(x, values + G::piece(16 * b + pos, s + col));
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        uint32_t a[4];
+                        halves_of_codes(__byte_perm(x[u], 0, 0x3120), a[0], a[1]);
+                        halves_of_codes(__byte_perm(x[2 + u], 0, 0x3120), a[2], a[3]);
+                        add(s + u, a);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < DH / 16; ++s) {
+                    uint32_t a[4];
+                    ldmatrix4_t(a, values + G::piece(16 * b + pos, 2 * s + col));
+                    add(s, a);
                 }
             }
         }
@@ -424,15 +453,15 @@ struct FmaWarp {
             for (int off = 1; off < 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             top = fmaxf(top, m[h]);
             const float base = top == kNone ? 0.0f : top;
-            const float keep = exp2f(m[h] - base);
+            const float keep = power2(m[h] - base);
             m[h] = top;
-            e[h] = on ? exp2f(s[h] - base) : 0.0f;
+            e[h] = power2(s[h] - base);
             l[h] = l[h] * keep + (side ? 0.0f : e[h]);
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) acc[h][i] *= keep;
         }
 #pragma unroll 4
-        for (int t = 0; t < kTile; ++t) {
+        for (int t = 0; t < G::kTile; ++t) {
             float v[kOwn];
             load_own(v, values, t, lane);
 #pragma unroll
@@ -492,7 +521,7 @@ template <typename T, typename W, int kBytes>
 __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(const AttendArgs p)
 {
     using G = typename W::G;
-    constexpr int kWarps = G::kWarps, kThreads = 32 * kWarps, kStages = G::kStages;
+    constexpr int kWarps = G::kWarps, kThreads = 32 * kWarps, kStages = G::kStages, kTile = G::kTile;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long scan[kWarps];
     __shared__ long long found_offset;
@@ -509,7 +538,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const int per = (p.seqs + kThreads - 1) / kThreads, s0 = min(tid * per, p.seqs), s1 = min(s0 + per, p.seqs);
         long long mine = 0;
         for (int s = s0; s < s1; ++s) {
-            const Span sp = span_of(p, s);
+            const Span sp = span_of<kTile>(p, s);
             mine += sp.t1 - sp.t0;
         }
         long long upto = mine;
@@ -537,7 +566,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             long long at = before;
             int s = s0;
             for (;;) {
-                const Span sp = span_of(p, s);
+                const Span sp = span_of<kTile>(p, s);
                 const long long n = (long long)(sp.t1 - sp.t0) * p.units;
                 if (x0 < at + n || s + 1 >= s1) break;
                 at += n;
@@ -552,13 +581,13 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     // ---- copies: the tiles that this warp will take, in order, kStages - 1 of them ahead ----
     const uint32_t ring = smem_at(smem) + warp * kStages * G::kStage;
     float* const join = reinterpret_cast<float*>(smem + kWarps * kStages * G::kStage);
-    Walk ahead, walk;
+    Walk<kTile> ahead, walk;
     ahead.begin(p, found_seq, found_offset, tiles);
     walk = ahead;
     int next_tile = ahead.at + warp;
-    bool more = true, on = false;                             // `on`: this lane's position (lane & 15) of the pending tile counts
+    bool more = true, on = false;                             // `on`: this lane's position (lane % kTile) of the pending tile counts
     int page = -1, in_page = 0;
-    long long head_at = 0;
+    const char *keys_of = nullptr, *values_of = nullptr;      // of the pending tile's head
     auto look_up = [&]() {                                    // the pending tile: which page each of its positions is on
         while (more && next_tile >= ahead.end) {
             more = ahead.next(p);
@@ -566,16 +595,21 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         }
         on = false;
         if (!more) return;
-        const int t = next_tile * kTile + (lane & 15);
+        const int t = next_tile * kTile + lane % kTile;
         on = t >= ahead.s.first && t < ahead.s.len;
         if (on) {
             const int column = p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size;
             in_page = t - column * p.page_size;
             page = p.table[(size_t)ahead.seq * p.table_ld + column];
         }
-        head_at = (ahead.unit / (p.units / p.kv_heads)) * p.head_stride;
+        const long long head_at = (ahead.unit / (p.units / p.kv_heads)) * p.head_stride;
+        keys_of = static_cast<const char*>(p.k) + head_at;
+        values_of = static_cast<const char*>(p.v) + head_at;
         next_tile += kWarps;
     };
+    constexpr int kRowsACopy = 32 / G::kPieces ? 32 / G::kPieces : 1;                  // rows that one copy of the warp covers
+    const int my_row = lane / G::kPieces, my_piece = lane % G::kPieces;
+    const long long my_at = my_row * p.token_stride + 16 * my_piece;
     auto issue = [&](int stage) {
         __syncwarp();                                         // everybody has read what the stage held
         if (on && (page < 0 || page >= p.pages)) {
@@ -583,16 +617,38 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             atomicCAS(p.status, 0, (int)GELO_ERR_INVALID);
         }
         const uint32_t who = __ballot_sync(0xffffffffu, on);
-        const long long at = on ? page * p.page_stride + in_page * p.token_stride + head_at : 0;
-        if (lane == 0) counts[warp][stage] = who & 0xffffu;
+        if (lane == 0) counts[warp][stage] = who;
+        const long long at = on ? page * p.page_stride + in_page * p.token_stride : 0;
         const uint32_t dst = ring + stage * G::kStage;
+        if (G::kPieces <= 32 && p.page_size % 16 == 0) {      // sixteen positions are neighbours on one page
+            const bool wanted = 16 * my_piece < p.dh * kBytes;
 #pragma unroll
-        for (int i = 0; i < kTile * G::kPieces / 32; ++i) {
-            const int idx = 32 * i + lane, row = idx / G::kPieces, c = idx % G::kPieces;
-            const long long from = __shfl_sync(0xffffffffu, at, row) + 16 * c;
-            const bool there = ((who >> row) & 1u) && 16 * c < p.dh * kBytes;
-            copy16(dst + G::piece(row, c), static_cast<const char*>(p.k) + (there ? from : 0), there);
-            copy16(dst + G::kHalf + G::piece(row, c), static_cast<const char*>(p.v) + (there ? from : 0), there);
+            for (int b = 0; b < kTile / 16; ++b) {
+                // the page is that of any position that counts; positions before it on the page may not count, but lie there
+                const uint32_t half = (who >> (16 * b)) & 0xffffu;
+                const int one = half ? __ffs(half) - 1 : 0;
+                const long long from = __shfl_sync(0xffffffffu, at, 16 * b + one) - (half ? one * p.token_stride : 0) + my_at;
+                const char *k = keys_of + from, *v = values_of + from;
+#pragma unroll
+                for (int i = 0; i < 16 / kRowsACopy; ++i) {
+                    const int row = i * kRowsACopy + my_row;
+                    const bool there = wanted && ((half >> row) & 1u);
+                    const uint32_t to = dst + G::piece(16 * b + row, my_piece);
+                    copy16(to, there ? k : p.k, there);
+                    copy16(to + G::kHalf, there ? v : p.v, there);
+                    k += kRowsACopy * p.token_stride;
+                    v += kRowsACopy * p.token_stride;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTile * G::kPieces / 32; ++i) {
+                const int idx = 32 * i + lane, row = idx / G::kPieces, c = idx % G::kPieces;
+                const long long from = __shfl_sync(0xffffffffu, at, row) + 16 * c;
+                const bool there = ((who >> row) & 1u) && 16 * c < p.dh * kBytes;
+                copy16(dst + G::piece(row, c), there ? keys_of + from : p.k, there);
+                copy16(dst + G::kHalf + G::piece(row, c), there ? values_of + from : p.v, there);
+            }
         }
     };
     look_up();
@@ -632,7 +688,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             const float base = my_top == kNone ? 0.0f : my_top;
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) {
-                factor[i][tid] = exp2f(tops[i][tid] - base);
+                factor[i][tid] = power2(tops[i][tid] - base);
                 my_total += factor[i][tid] * totals[i][tid];
             }
             totals[0][tid] = my_total;
@@ -690,7 +746,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
 #pragma unroll 4
             for (int a = first_cta; a <= last_cta; ++a) {
                 const float* from = p.slots + (size_t)(2 * a + (a == first_cta ? 1 : 0)) * kSlotFloats;
-                const float f = exp2f(__ldcg(from + 16 * 256 + h) - base);
+                const float f = power2(__ldcg(from + 16 * 256 + h) - base);
                 const float4 v = __ldcg(reinterpret_cast<const float4*>(from + h * 256 + c));
                 total = fmaf(f, __ldcg(from + 16 * 256 + 16 + h), total);
                 sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
