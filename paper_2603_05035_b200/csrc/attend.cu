@@ -21,6 +21,7 @@ namespace gelo {
 namespace {
 
 constexpr int kMaxCtas = 320;
+constexpr int kLeast = 4;                                     // tiles that a warp takes where heads are cut
 constexpr int kMaxParts = 64;                                 // a head's sums come from no more than about so many CTAs
 constexpr int kSlotFloats = 16 * 256 + 32;                    // sums of 16 heads, their maxima, their totals
 constexpr float kNone = -INFINITY;
@@ -39,6 +40,12 @@ struct AttendArgs {
     int kv_heads, heads_a_unit, units;                        // units: heads_a_unit query heads of one key-value head each, per sequence
     float scale, v_scale;                                     // scale: of the logits, the keys' scale included
 };
+
+// a / b of non-negative numbers; nearly always both are small
+__device__ __forceinline__ long long quotient(long long a, long long b)
+{
+    return ((a | b) >> 31) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
 
 // The positions that count of one sequence, and its tiles
 struct Span { int first, len, t0, t1; };
@@ -71,7 +78,7 @@ struct Walk {
         seq = seq0;
         s = span_of<kTile>(p, seq);
         const int n = s.t1 - s.t0;
-        unit = (int)(offset / n);
+        unit = (int)quotient(offset, n);
         at = s.t0 + (int)(offset - (long long)unit * n);
         end = at + (int)min((long long)(s.t1 - at), tiles);
         left = tiles - (end - at);
@@ -156,6 +163,7 @@ __device__ __forceinline__ void halves_of_codes(uint32_t four, uint32_t& low, ui
 // rows' pieces of one column lie in different banks.
 template <int DH, int kBytes>
 struct Tiles {
+    static constexpr int kWidth = DH;
     static constexpr int kRow = DH * kBytes;                  // bytes
     static constexpr int kTile = kRow <= 128 ? 32 : 16;       // positions
     static constexpr int kPieces = kRow / 16;                 // of a row
@@ -171,6 +179,32 @@ struct Tiles {
     __device__ static __forceinline__ uint32_t piece(int row, int c)                   // byte offset of piece c of a row
     {
         return kPieces >= 8 ? row * kRow + ((c ^ (row & 7)) << 4) : row * kRow + ((c ^ ((row >> 1) & (kPieces - 1))) << 4);
+    }
+};
+
+// What the warps know of a segment's heads: the maximum of each warp's logits (times log2 e) and its total relative to that
+template <int kHeads, int kWarps>
+struct Joint {
+    float tops[kWarps][kHeads], totals[kWarps][kHeads];
+    __device__ __forceinline__ float top(int h) const
+    {
+        float t = kNone;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) t = fmaxf(t, tops[w][h]);
+        return t;
+    }
+    __device__ __forceinline__ float base(int h) const
+    {
+        const float t = top(h);
+        return t == kNone ? 0.0f : t;
+    }
+    __device__ __forceinline__ float total(int h) const
+    {
+        const float b = base(h);
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) sum = fmaf(power2(tops[w][h] - b), totals[w][h], sum);
+        return sum;
     }
 };
 
@@ -190,25 +224,46 @@ struct MmaWarp {
     float acc[DH / 16][NT][4];
     float m[NT][2], l[NT][2], scale[NT][2];
 
-    // heads [0, heads) of the unit; q points at the first one's components
-    __device__ __forceinline__ void begin(const AttendArgs& p, const T* q, int heads, int lane)
+    static constexpr int kStaged = 0;                         // floats of shared memory for q
+
+    // Asks for the q of a segment's heads; q points at the first one's components.  What arrives is taken up by begin().
+    __device__ __forceinline__ void fetch(const AttendArgs& p, const T* q, int heads, int lane)
     {
         const int t = lane & 3;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int h = 8 * n + (lane >> 2);
             const T* row = q + (size_t)h * p.dh;
+#pragma unroll
+            for (int s = 0; s < DH / 16; ++s) {
+                if constexpr (kCodes) {
+                    const int c = 16 * s + 4 * t;             // the components that stand where a code tile's row has them
+                    const uint2 v = h < heads && c < p.dh ? *reinterpret_cast<const uint2*>(row + c) : make_uint2(0u, 0u);
+                    qf[s][n][0] = v.x;
+                    qf[s][n][1] = v.y;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int c = 16 * s + 2 * t + 8 * j;
+                        qf[s][n][j] = h < heads && c < p.dh ? *reinterpret_cast<const uint32_t*>(row + c) : 0u;
+                    }
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void stage(float*, int, int) {}
+    __device__ __forceinline__ void begin(const AttendArgs& p, const float*, int, int lane)
+    {
+        const int t = lane & 3;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             float factor = 1.0f;
             if constexpr (kCodes) {
-                float v[DH / 16][4], top = 0.0f;
+                float top = 0.0f;
 #pragma unroll
                 for (int s = 0; s < DH / 16; ++s)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int c = 16 * s + 4 * t + j;
-                        v[s][j] = h < heads && c < p.dh ? widen_at(row, c) : 0.0f;
-                        top = fmaxf(top, fabsf(v[s][j]));
-                    }
+                    for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(widen_at(reinterpret_cast<const T*>(qf[s][n]), j)));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 int e = 0;
@@ -218,14 +273,9 @@ struct MmaWarp {
 #pragma unroll
                 for (int s = 0; s < DH / 16; ++s)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) qf[s][n][j] = pack2<M>(v[s][2 * j] * down, v[s][2 * j + 1] * down);
-            } else {
-#pragma unroll
-                for (int s = 0; s < DH / 16; ++s)
-#pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const int c = 16 * s + 2 * t + 8 * j;
-                        qf[s][n][j] = h < heads && c < p.dh ? *reinterpret_cast<const uint32_t*>(row + c) : 0u;
+                        const T* two = reinterpret_cast<const T*>(&qf[s][n][j]);
+                        qf[s][n][j] = pack2<M>(widen_at(two, 0) * down, widen_at(two, 1) * down);
                     }
             }
             // columns 2t and 2t + 1 of a product are heads whose q other lanes hold
@@ -380,8 +430,8 @@ struct MmaWarp {
                 }
             }
     }
-    // sums of heads [h0, h0 + 4) times factor[head], head-major with the join's pitch
-    __device__ __forceinline__ void sums(float* out, const float* factor, int h0, int lane)
+    // sums of heads [h0, h0 + kJoinHeads) brought to the maximum of all warps, head-major with the join's pitch
+    __device__ __forceinline__ void sums(float* out, const Joint<kHeads, G::kWarps>& all, int h0, int lane)
     {
         const int r = lane >> 2, t = lane & 3;
 #pragma unroll
@@ -389,8 +439,8 @@ struct MmaWarp {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int h = 8 * n + 2 * t + j;
-                if (h < h0 || h >= h0 + 4) continue;
-                const float f = factor[h];
+                if (h < h0 || h >= h0 + G::kJoinHeads) continue;
+                const float f = power2(m[n][j] - all.base(h));
                 float* dst = out + (h - h0) * G::kJoinPitch;
 #pragma unroll
                 for (int s = 0; s < DH / 16; ++s) {
@@ -402,22 +452,43 @@ struct MmaWarp {
 };
 
 // ---- products of a warp on an fp32 tile: multiply-adds ------------------------------------------------------
-// Logits: two lanes per position, half the components each, a key's piece in registers for all heads.  Sums: a lane owns DH / 32 components.
-template <int DH>
+// Logits: two lanes per position, every other piece of a row each, a key's piece in registers for all H heads, q in shared memory.  Sums: a lane owns
+// DH / 32 components.
+template <int DH, int H>
 struct FmaWarp {
     using G = Tiles<DH, 4>;
-    static constexpr int kHeads = 8;
+    static constexpr int kHeads = H;
     static constexpr int kOwn = DH / 32;
+    static constexpr int kThreads = 32 * G::kWarps;
+    static constexpr int kStaged = H * DH;
+    static constexpr int kMine = (kStaged + kThreads - 1) / kThreads;
     const float* q;
-    int heads, dh, group;
-    float acc[kHeads][kOwn];
-    float m[kHeads], l[kHeads], scale;
+    float held[kMine];
+    float acc[H][kOwn];
+    float m[H], l[H], scale;
 
-    __device__ __forceinline__ void begin(const AttendArgs& p, const float* q_, int heads_, int)
+    __device__ __forceinline__ void fetch(const AttendArgs& p, const float* from, int heads, int)
     {
-        q = q_; heads = heads_; dh = p.dh; scale = p.scale * kLog2e;
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
+        for (int i = 0; i < kMine; ++i) {
+            const int at = i * kThreads + threadIdx.x, h = at / DH, c = at % DH;
+            held[i] = h < heads && c < p.dh ? from[(size_t)h * p.dh + c] : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void stage(float* staged, int, int)
+    {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int at = i * kThreads + threadIdx.x;
+            if (kStaged % kThreads == 0 || at < kStaged) staged[at] = held[i];
+        }
+    }
+    __device__ __forceinline__ void begin(const AttendArgs& p, const float* staged, int, int)
+    {
+        q = staged;
+        scale = p.scale * kLog2e;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
             m[h] = kNone;
             l[h] = 0.0f;
 #pragma unroll
@@ -427,25 +498,24 @@ struct FmaWarp {
     __device__ __forceinline__ void tile(uint32_t keys, uint32_t values, uint32_t counts, int lane)
     {
         const int row = lane & 15, side = lane >> 4;
-        float s[kHeads];
+        float s[H];
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) s[h] = 0.0f;
-        for (int c = side; c < dh / 4; c += 2) {
+        for (int h = 0; h < H; ++h) s[h] = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < DH / 8; ++i) {
+            const int c = 2 * i + side;
             float4 k4;
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k4.x), "=f"(k4.y), "=f"(k4.z), "=f"(k4.w) : "r"(keys + G::piece(row, c)) : "memory");
 #pragma unroll
-            for (int h = 0; h < kHeads; ++h) {
-                if (h < heads) {
-                    const float4 q4 = *reinterpret_cast<const float4*>(q + (size_t)h * dh + 4 * c);
-                    s[h] = fmaf(k4.x, q4.x, fmaf(k4.y, q4.y, fmaf(k4.z, q4.z, fmaf(k4.w, q4.w, s[h]))));
-                }
+            for (int h = 0; h < H; ++h) {
+                const float4 q4 = *reinterpret_cast<const float4*>(q + h * DH + 4 * c);
+                s[h] = fmaf(k4.x, q4.x, fmaf(k4.y, q4.y, fmaf(k4.z, q4.z, fmaf(k4.w, q4.w, s[h]))));
             }
         }
         const bool on = (counts >> row) & 1u;
-        float e[kHeads];
+        float e[H];
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-            if (h >= heads) break;
+        for (int h = 0; h < H; ++h) {
             s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
             s[h] = on ? s[h] * scale : kNone;
             float top = s[h];
@@ -456,17 +526,16 @@ struct FmaWarp {
             const float keep = power2(m[h] - base);
             m[h] = top;
             e[h] = power2(s[h] - base);
-            l[h] = l[h] * keep + (side ? 0.0f : e[h]);
+            l[h] = fmaf(l[h], keep, side ? 0.0f : e[h]);
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) acc[h][i] *= keep;
         }
-#pragma unroll 4
+#pragma unroll 8
         for (int t = 0; t < G::kTile; ++t) {
             float v[kOwn];
             load_own(v, values, t, lane);
 #pragma unroll
-            for (int h = 0; h < kHeads; ++h) {
-                if (h >= heads) break;
+            for (int h = 0; h < H; ++h) {
                 const float w = __shfl_sync(0xffffffffu, e[h], t);
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i) acc[h][i] = fmaf(w, v[i], acc[h][i]);
@@ -489,7 +558,7 @@ struct FmaWarp {
     __device__ __forceinline__ void statistics(float* tops, float* totals, int lane)
     {
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
+        for (int h = 0; h < H; ++h) {
             float sum = l[h];
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
@@ -499,22 +568,28 @@ struct FmaWarp {
             }
         }
     }
-    __device__ __forceinline__ void sums(float* out, const float* factor, int h0, int lane)
+    __device__ __forceinline__ void sums(float* out, const Joint<kHeads, G::kWarps>& all, int h0, int lane)
     {
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) {
-            if (h < h0 || h >= h0 + 4) continue;
+        for (int h = 0; h < H; ++h) {
+            if (h < h0 || h >= h0 + G::kJoinHeads) continue;
+            const float f = power2(m[h] - all.base(h));
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i) out[(h - h0) * G::kJoinPitch + component(lane, i)] = acc[h][i] * factor[h];
+            for (int i = 0; i < kOwn; ++i) out[(h - h0) * G::kJoinPitch + component(lane, i)] = acc[h][i] * f;
         }
     }
 };
 
-template <typename T, typename W>
-__device__ __forceinline__ void write_result(const AttendArgs& p, int seq, int head, int c, float sum, float total)
+// Four neighbouring components of a result
+template <typename T>
+__device__ __forceinline__ void write_result(const AttendArgs& p, int seq, int head, int c, float4 sum, float total)
 {
-    const float o = total > 0.0f || total != total ? sum / total * p.v_scale : 0.0f;
-    round_to(o, static_cast<T*>(p.o) + (size_t)seq * p.ldo + (size_t)head * p.dh + c);
+    const float f = total > 0.0f || total != total ? __fdiv_rn(p.v_scale, total) : 0.0f;
+    __align__(16) T o[4];
+    round_to(sum.x * f, o); round_to(sum.y * f, o + 1); round_to(sum.z * f, o + 2); round_to(sum.w * f, o + 3);
+    T* dst = static_cast<T*>(p.o) + (size_t)seq * p.ldo + (size_t)head * p.dh + c;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(o);
+    else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(o);
 }
 
 template <typename T, typename W, int kBytes>
@@ -527,7 +602,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     __shared__ long long found_offset;
     __shared__ int found_seq, last;
     __shared__ uint32_t counts[kWarps][kStages];
-    __shared__ float tops[kWarps][W::kHeads], totals[kWarps][W::kHeads], factor[kWarps][W::kHeads];
+    __shared__ Joint<W::kHeads, kWarps> joint[2];             // of this segment, and of the one before or behind
+    __shared__ __align__(16) float staged[W::kStaged ? W::kStaged : 1];
     chain_next();
     chain_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
@@ -556,8 +632,9 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             all += scan[w];
         }
         const long long total = all * p.units;
-        // a tile for every warp at least, and no head cut into many more than kMaxParts pieces
-        share = max(max((total + gridDim.x - 1) / gridDim.x, (long long)kWarps), (all / p.seqs + kMaxParts - 1) / kMaxParts);
+        // kLeast tiles for every warp, or a whole average head, since what a cut costs is more; and no head in many more than kMaxParts pieces
+        const long long average = quotient(all + p.seqs - 1, p.seqs);
+        share = max(max(quotient(total + gridDim.x - 1, gridDim.x), min((long long)kLeast * kWarps, average)), (average + kMaxParts - 1) / kMaxParts);
         x0 = cta * share;
         tiles = min(share, total - x0);
         if (tiles <= 0) return;
@@ -661,13 +738,20 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
 
     // ---- segments ----
     W w;
-    int put = kStages - 1, get = 0;
+    int first_head, heads;                                    // of the segment
+    auto fetch = [&](const Walk<kTile>& at) {
+        const int per_kv = p.units / p.kv_heads, kv_head = at.unit / per_kv, head0 = (at.unit - kv_head * per_kv) * p.heads_a_unit;
+        heads = min(p.heads_a_unit, p.group - head0);
+        first_head = kv_head * p.group + head0;
+        w.fetch(p, static_cast<const T*>(p.q) + (size_t)at.seq * p.ldq + (size_t)first_head * p.dh, heads, lane);
+    };
+    fetch(walk);
+    w.stage(staged, tid, lane);
+    if constexpr (W::kStaged > 0) __syncthreads();
+    int put = kStages - 1, get = 0, turn = 0;
     long long x = x0;                                         // where the segment begins
-    for (bool go = true; go; x += walk.end - walk.at, go = walk.next(p)) {
-        const int part_of_kv = p.units / p.kv_heads;
-        const int kv_head = walk.unit / part_of_kv, head0 = (walk.unit - kv_head * part_of_kv) * p.heads_a_unit;
-        const int heads = min(p.heads_a_unit, p.group - head0), first_head = kv_head * p.group + head0;
-        w.begin(p, static_cast<const T*>(p.q) + (size_t)walk.seq * p.ldq + (size_t)first_head * p.dh, heads, lane);
+    for (;; turn ^= 1) {
+        w.begin(p, staged, tid, lane);
         for (int t = walk.at + warp; t < walk.end; t += kWarps) {
             if (more) issue(put);
             copies_end();
@@ -678,84 +762,94 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             put = put + 1 == kStages ? 0 : put + 1;
             get = get + 1 == kStages ? 0 : get + 1;
         }
-        // the warps' sums, brought to one maximum
-        w.statistics(tops[warp], totals[warp], lane);
+        // The warps' sums, brought to one maximum.  The next segment's q is on its way meanwhile, and what the warps exchange
+        // alternates between two places: a warp that is through may begin the next segment before the others are.
+        Joint<W::kHeads, kWarps>& all = joint[turn];
+        w.statistics(all.tops[warp], all.totals[warp], lane);
+        const Walk<kTile> done = walk;
+        const int done_head = first_head, done_heads = heads;
+        const bool go = walk.next(p);
+        if (go) fetch(walk);
         __syncthreads();
-        float my_top = kNone, my_total = 0.0f;                // of head tid, where there is one
-        if (tid < heads) {
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) my_top = fmaxf(my_top, tops[i][tid]);
-            const float base = my_top == kNone ? 0.0f : my_top;
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) {
-                factor[i][tid] = power2(tops[i][tid] - base);
-                my_total += factor[i][tid] * totals[i][tid];
-            }
-            totals[0][tid] = my_total;
-        }
-        const int n = walk.s.t1 - walk.s.t0;
-        const long long unit_at = x - (walk.at - walk.s.t0);
-        const bool whole = walk.end - walk.at == n;
-        const int first_cta = whole ? cta : (int)(unit_at / share), last_cta = whole ? cta : (int)((unit_at + n - 1) / share);
+        if (go) w.stage(staged, tid, lane);
+        const int n = done.s.t1 - done.s.t0;
+        const bool whole = done.end - done.at == n;
+        const long long unit_at = x - (done.at - done.s.t0);
+        const int first_cta = whole ? cta : (int)quotient(unit_at, share), last_cta = whole ? cta : (int)quotient(unit_at + n - 1, share);
         float* slot = p.slots + (size_t)(2 * cta + (first_cta == cta ? 1 : 0)) * kSlotFloats;
-        if (tid < heads) {
+        if (tid < done_heads) {
+            const float total = all.total(tid);
             if (!whole) {
-                slot[16 * 256 + tid] = my_top;
-                slot[16 * 256 + 16 + tid] = my_total;
+                slot[16 * 256 + tid] = all.top(tid);
+                slot[16 * 256 + 16 + tid] = total;
             } else if (p.lse) {
-                p.lse[(size_t)walk.seq * p.q_heads + first_head + tid] = (my_top == kNone ? 0.0f : my_top * kLn2) + logf(my_total);
+                p.lse[(size_t)done.seq * p.q_heads + done_head + tid] = all.base(tid) * kLn2 + logf(total);
             }
         }
-        __syncthreads();
-        for (int h0 = 0; h0 < heads; h0 += G::kJoinHeads) {
-            w.sums(join + warp * G::kJoinHeads * G::kJoinPitch, factor[warp], h0, lane);
+        constexpr int kQuads = G::kWidth / 4, kRows = kThreads / kQuads;                      // a row of threads adds up a head, four components each
+        const int c = 4 * (tid % kQuads), my_h = tid / kQuads;
+        for (int h0 = 0; h0 < done_heads; h0 += G::kJoinHeads) {
+            if (h0 > 0) __syncthreads();
+            w.sums(join + warp * G::kJoinHeads * G::kJoinPitch, all, h0, lane);
             __syncthreads();
-            const int some = min(heads - h0, G::kJoinHeads);
-            for (int i = tid; i < some * p.dh; i += kThreads) {
-                const int h = i / p.dh, c = i - h * p.dh;
-                float sum = 0.0f;
+            const int some = min(done_heads - h0, G::kJoinHeads);
+            for (int h = my_h; h < some && c < p.dh; h += kRows) {
+                float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                for (int j = 0; j < kWarps; ++j) sum += join[(j * G::kJoinHeads + h) * G::kJoinPitch + c];
-                if (whole) write_result<T, W>(p, walk.seq, first_head + h0 + h, c, sum, totals[0][h0 + h]);
-                else slot[(h0 + h) * 256 + c] = sum;
+                for (int j = 0; j < kWarps; ++j) {
+                    const float4 v = *reinterpret_cast<const float4*>(join + (j * G::kJoinHeads + h) * G::kJoinPitch + c);
+                    sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+                }
+                if (whole) write_result<T>(p, done.seq, done_head + h0 + h, c, sum, all.total(h0 + h));
+                else *reinterpret_cast<float4*>(slot + (h0 + h) * 256 + c) = sum;
+            }
+        }
+        if (!whole) {
+            // a head that several CTAs share: the last one to arrive adds up, in the order of the CTAs
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                const int before = atomicAdd(p.arrived + first_cta, 1);
+                last = before == last_cta - first_cta;
+                if (last) p.arrived[first_cta] = 0;
             }
             __syncthreads();
-        }
-        if (whole) continue;
-
-        // ---- a head that several CTAs share: the last one to arrive adds up ----
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-            const int parts = last_cta - first_cta + 1;
-            const int before = atomicAdd(p.arrived + first_cta, 1);
-            last = before == parts - 1;
-            if (last) p.arrived[first_cta] = 0;
-        }
-        __syncthreads();
-        if (!last) continue;
-        __threadfence();
-        for (int i = tid; i < heads * (p.dh / 4); i += kThreads) {
-            const int h = i / (p.dh / 4), c = 4 * (i - h * (p.dh / 4));
-            float top = kNone;
-            for (int a = first_cta; a <= last_cta; ++a)
-                top = fmaxf(top, __ldcg(p.slots + (size_t)(2 * a + (a == first_cta ? 1 : 0)) * kSlotFloats + 16 * 256 + h));
-            const float base = top == kNone ? 0.0f : top;
-            float total = 0.0f;
-            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-            for (int a = first_cta; a <= last_cta; ++a) {
-                const float* from = p.slots + (size_t)(2 * a + (a == first_cta ? 1 : 0)) * kSlotFloats;
-                const float f = power2(__ldcg(from + 16 * 256 + h) - base);
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(from + h * 256 + c));
-                total = fmaf(f, __ldcg(from + 16 * 256 + 16 + h), total);
-                sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
-            }
-            const float four[4] = {sum.x, sum.y, sum.z, sum.w};
+            if (last) {
+                __threadfence();
+                for (int h = my_h; h < done_heads && c < p.dh; h += kRows) {
+                    float top = kNone, total = 0.0f;
+                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    for (int a = first_cta; a <= last_cta; a += 4) {
+                        float t[4], l[4];
+                        float4 v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) write_result<T, W>(p, walk.seq, first_head + h, c + j, four[j], total);
-            if (p.lse && c == 0) p.lse[(size_t)walk.seq * p.q_heads + first_head + h] = base * kLn2 + logf(total);
+                        for (int i = 0; i < 4; ++i) {
+                            const int b = min(a + i, last_cta);
+                            const float* from = p.slots + (size_t)(2 * b + (b == first_cta ? 1 : 0)) * kSlotFloats;
+                            t[i] = a + i <= last_cta ? __ldcg(from + 16 * 256 + h) : kNone;
+                            l[i] = __ldcg(from + 16 * 256 + 16 + h);
+                            v[i] = __ldcg(reinterpret_cast<const float4*>(from + h * 256 + c));
+                        }
+                        const float higher = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), top);
+                        const float base = higher == kNone ? 0.0f : higher, keep = power2(top - base);
+                        top = higher;
+                        total *= keep;
+                        sum.x *= keep; sum.y *= keep; sum.z *= keep; sum.w *= keep;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float f = power2(t[i] - base);
+                            if (a + i > last_cta) continue;
+                            total = fmaf(f, l[i], total);
+                            sum.x = fmaf(f, v[i].x, sum.x); sum.y = fmaf(f, v[i].y, sum.y); sum.z = fmaf(f, v[i].z, sum.z); sum.w = fmaf(f, v[i].w, sum.w);
+                        }
+                    }
+                    write_result<T>(p, done.seq, done_head + h, c, sum, total);
+                    if (p.lse && c == 0) p.lse[(size_t)done.seq * p.q_heads + done_head + h] = (top == kNone ? 0.0f : top * kLn2) + logf(total);
+                }
+            }
         }
+        if (!go) break;
+        x += done.end - done.at;
     }
 }
 
@@ -788,6 +882,14 @@ int launch_mma(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
     return launch_as<T, MmaWarp<T, kCodes, 256, 2>, kBytes>(ctx, p, st);
 }
 
+template <int H>
+int launch_fma(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
+{
+    if (p.dh <= 64) return launch_as<float, FmaWarp<64, H>, 4>(ctx, p, st);
+    if (p.dh <= 128) return launch_as<float, FmaWarp<128, H>, 4>(ctx, p, st);
+    return launch_as<float, FmaWarp<256, H>, 4>(ctx, p, st);
+}
+
 }  // namespace
 
 size_t attend_workspace_bytes() { return (size_t)2 * kMaxCtas * kSlotFloats * sizeof(float); }
@@ -811,9 +913,9 @@ int launch_paged_attention(gelo_ctx* ctx, const gelo_kv_cache& kv, const void* q
     p.window = window; p.scale = scale * kv.k_scale; p.v_scale = kv.v_scale;
     if (dtype == GELO_BF16) return codes ? launch_mma<__nv_bfloat16, true>(ctx, p, st) : launch_mma<__nv_bfloat16, false>(ctx, p, st);
     if (dtype == GELO_F16) return codes ? launch_mma<__half, true>(ctx, p, st) : launch_mma<__half, false>(ctx, p, st);
-    if (p.dh <= 64) return launch_as<float, FmaWarp<64>, 4>(ctx, p, st);
-    if (p.dh <= 128) return launch_as<float, FmaWarp<128>, 4>(ctx, p, st);
-    return launch_as<float, FmaWarp<256>, 4>(ctx, p, st);
+    if (p.group == 1) return launch_fma<1>(ctx, p, st);
+    if (p.group <= 4) return launch_fma<4>(ctx, p, st);
+    return launch_fma<8>(ctx, p, st);
 }
 
 }  // namespace gelo
