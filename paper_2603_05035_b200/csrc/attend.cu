@@ -592,6 +592,23 @@ __device__ __forceinline__ void write_result(const AttendArgs& p, int seq, int h
     else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(o);
 }
 
+// (top, total, sum) += the part (t, l, v), both brought to the maximum `higher` of all that is being added; `fresh` begins with the part alone
+__device__ __forceinline__ void add_part(float& top, float& total, float4& sum, float higher, float t, float l, float4 v, bool fresh)
+{
+    const float f = power2(t - (higher == kNone ? 0.0f : higher));
+    if (fresh) {
+        total = f * l;
+        sum = make_float4(f * v.x, f * v.y, f * v.z, f * v.w);
+    } else {
+        total = fmaf(f, l, total);
+        sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+    }
+    top = higher;
+}
+
+// A head that this CTA shares with others: those are CTAs first .. last, which leave their sums in slots
+struct Cut { int first, last, seq, head, heads; };
+
 template <typename T, typename W, int kBytes>
 __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(const AttendArgs p)
 {
@@ -600,7 +617,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long scan[kWarps];
     __shared__ long long found_offset;
-    __shared__ int found_seq, last;
+    __shared__ int found_seq, last[2];
     __shared__ uint32_t counts[kWarps][kStages];
     __shared__ Joint<W::kHeads, kWarps> joint[2];             // of this segment, and of the one before or behind
     __shared__ __align__(16) float staged[W::kStaged ? W::kStaged : 1];
@@ -661,41 +678,58 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     Walk<kTile> ahead, walk;
     ahead.begin(p, found_seq, found_offset, tiles);
     walk = ahead;
+    W w;
+    int first_head, heads;                                    // of the segment
+    auto fetch = [&](const Walk<kTile>& at) {
+        const int per_kv = p.units / p.kv_heads, kv_head = at.unit / per_kv, head0 = (at.unit - kv_head * per_kv) * p.heads_a_unit;
+        heads = min(p.heads_a_unit, p.group - head0);
+        first_head = kv_head * p.group + head0;
+        w.fetch(p, static_cast<const T*>(p.q) + (size_t)at.seq * p.ldq + (size_t)first_head * p.dh, heads, lane);
+    };
+    fetch(walk);
     int next_tile = ahead.at + warp;
-    bool more = true, on = false;                             // `on`: this lane's position (lane % kTile) of the pending tile counts
-    int page = -1, in_page = 0;
-    const char *keys_of = nullptr, *values_of = nullptr;      // of the pending tile's head
-    auto look_up = [&]() {                                    // the pending tile: which page each of its positions is on
+    bool more = true;
+    // The next two tiles whose copies have not been asked for: the page that each position (lane % kTile) is on is looked up that far ahead.
+    struct Pending {
+        const char *keys, *values;                            // of the tile's head
+        int page, in_page;
+        bool any, on;                                         // there is a tile; this lane's position of it counts
+    } near = {nullptr, nullptr, 0, 0, false, false}, far = near;
+    constexpr int kRowsACopy = 32 / G::kPieces ? 32 / G::kPieces : 1;                  // rows that one copy of the warp covers
+    const int my_row = lane / G::kPieces, my_piece = lane % G::kPieces;
+    const long long my_at = my_row * p.token_stride + 16 * my_piece;
+    auto copy_tile = [&](int stage) {                         // asks for the copies of the next tile and looks up the one after the one behind it
+        const Pending t = near;
+        near = far;
         while (more && next_tile >= ahead.end) {
             more = ahead.next(p);
             next_tile = ahead.at + warp;
         }
-        on = false;
-        if (!more) return;
-        const int t = next_tile * kTile + lane % kTile;
-        on = t >= ahead.s.first && t < ahead.s.len;
-        if (on) {
-            const int column = p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size;
-            in_page = t - column * p.page_size;
-            page = p.table[(size_t)ahead.seq * p.table_ld + column];
+        far.any = more;
+        far.on = false;
+        if (more) {
+            const int at = next_tile * kTile + lane % kTile;
+            far.on = at >= ahead.s.first && at < ahead.s.len;
+            if (far.on) {
+                const int column = p.page_shift >= 0 ? at >> p.page_shift : at / p.page_size;
+                far.in_page = at - column * p.page_size;
+                far.page = p.table[(size_t)ahead.seq * p.table_ld + column];
+            }
+            const long long head_at = (ahead.unit / (p.units / p.kv_heads)) * p.head_stride;
+            far.keys = static_cast<const char*>(p.k) + head_at;
+            far.values = static_cast<const char*>(p.v) + head_at;
+            next_tile += kWarps;
         }
-        const long long head_at = (ahead.unit / (p.units / p.kv_heads)) * p.head_stride;
-        keys_of = static_cast<const char*>(p.k) + head_at;
-        values_of = static_cast<const char*>(p.v) + head_at;
-        next_tile += kWarps;
-    };
-    constexpr int kRowsACopy = 32 / G::kPieces ? 32 / G::kPieces : 1;                  // rows that one copy of the warp covers
-    const int my_row = lane / G::kPieces, my_piece = lane % G::kPieces;
-    const long long my_at = my_row * p.token_stride + 16 * my_piece;
-    auto issue = [&](int stage) {
+        if (!t.any) return;
         __syncwarp();                                         // everybody has read what the stage held
-        if (on && (page < 0 || page >= p.pages)) {
+        bool on = t.on;
+        if (on && (t.page < 0 || t.page >= p.pages)) {
             on = false;
             atomicCAS(p.status, 0, (int)GELO_ERR_INVALID);
         }
         const uint32_t who = __ballot_sync(0xffffffffu, on);
         if (lane == 0) counts[warp][stage] = who;
-        const long long at = on ? page * p.page_stride + in_page * p.token_stride : 0;
+        const long long at = on ? t.page * p.page_stride + t.in_page * p.token_stride : 0;
         const uint32_t dst = ring + stage * G::kStage;
         if (G::kPieces <= 32 && p.page_size % 16 == 0) {      // sixteen positions are neighbours on one page
             const bool wanted = 16 * my_piece < p.dh * kBytes;
@@ -705,7 +739,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 const uint32_t half = (who >> (16 * b)) & 0xffffu;
                 const int one = half ? __ffs(half) - 1 : 0;
                 const long long from = __shfl_sync(0xffffffffu, at, 16 * b + one) - (half ? one * p.token_stride : 0) + my_at;
-                const char *k = keys_of + from, *v = values_of + from;
+                const char *k = t.keys + from, *v = t.values + from;
 #pragma unroll
                 for (int i = 0; i < 16 / kRowsACopy; ++i) {
                     const int row = i * kRowsACopy + my_row;
@@ -723,43 +757,34 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 const int idx = 32 * i + lane, row = idx / G::kPieces, c = idx % G::kPieces;
                 const long long from = __shfl_sync(0xffffffffu, at, row) + 16 * c;
                 const bool there = ((who >> row) & 1u) && 16 * c < p.dh * kBytes;
-                copy16(dst + G::piece(row, c), there ? keys_of + from : p.k, there);
-                copy16(dst + G::kHalf + G::piece(row, c), there ? values_of + from : p.v, there);
+                copy16(dst + G::piece(row, c), there ? t.keys + from : p.k, there);
+                copy16(dst + G::kHalf + G::piece(row, c), there ? t.values + from : p.v, there);
             }
         }
     };
-    look_up();
-#pragma unroll 1
-    for (int s = 0; s < kStages - 1; ++s) {
-        if (more) issue(s);
-        copies_end();
-        look_up();
-    }
 
     // ---- segments ----
-    W w;
-    int first_head, heads;                                    // of the segment
-    auto fetch = [&](const Walk<kTile>& at) {
-        const int per_kv = p.units / p.kv_heads, kv_head = at.unit / per_kv, head0 = (at.unit - kv_head * per_kv) * p.heads_a_unit;
-        heads = min(p.heads_a_unit, p.group - head0);
-        first_head = kv_head * p.group + head0;
-        w.fetch(p, static_cast<const T*>(p.q) + (size_t)at.seq * p.ldq + (size_t)first_head * p.dh, heads, lane);
-    };
-    fetch(walk);
     w.stage(staged, tid, lane);
     if constexpr (W::kStaged > 0) __syncthreads();
-    int put = kStages - 1, get = 0, turn = 0;
+    Cut cuts[2] = {};
+    constexpr int kQuads = G::kWidth / 4, kRows = kThreads / kQuads;                          // a row of threads adds up a head, four components each
+    const int c = 4 * (tid % kQuads), my_h = tid / kQuads;
+    int put = 0, get = 0, turn = 0, lead = -2;                // lead: tiles asked for and not used (the first two rounds only look up)
     long long x = x0;                                         // where the segment begins
     for (;; turn ^= 1) {
         w.begin(p, staged, tid, lane);
         for (int t = walk.at + warp; t < walk.end; t += kWarps) {
-            if (more) issue(put);
-            copies_end();
-            look_up();
+#pragma unroll 1
+            for (; lead < kStages; ++lead) {
+                copy_tile(put);
+                if (lead < 0) continue;
+                copies_end();
+                put = put + 1 == kStages ? 0 : put + 1;
+            }
             copies_wait<kStages - 1>();
             __syncwarp();
             w.tile(ring + get * G::kStage, ring + get * G::kStage + G::kHalf, counts[warp][get], lane);
-            put = put + 1 == kStages ? 0 : put + 1;
+            --lead;
             get = get + 1 == kStages ? 0 : get + 1;
         }
         // The warps' sums, brought to one maximum.  The next segment's q is on its way meanwhile, and what the warps exchange
@@ -780,14 +805,11 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         if (tid < done_heads) {
             const float total = all.total(tid);
             if (!whole) {
-                slot[16 * 256 + tid] = all.top(tid);
-                slot[16 * 256 + 16 + tid] = total;
+                *reinterpret_cast<float2*>(slot + 16 * 256 + 2 * tid) = make_float2(all.top(tid), total);
             } else if (p.lse) {
                 p.lse[(size_t)done.seq * p.q_heads + done_head + tid] = all.base(tid) * kLn2 + logf(total);
             }
         }
-        constexpr int kQuads = G::kWidth / 4, kRows = kThreads / kQuads;                      // a row of threads adds up a head, four components each
-        const int c = 4 * (tid % kQuads), my_h = tid / kQuads;
         for (int h0 = 0; h0 < done_heads; h0 += G::kJoinHeads) {
             if (h0 > 0) __syncthreads();
             w.sums(join + warp * G::kJoinHeads * G::kJoinPitch, all, h0, lane);
@@ -805,51 +827,86 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             }
         }
         if (!whole) {
-            // a head that several CTAs share: the last one to arrive adds up, in the order of the CTAs
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const int before = atomicAdd(p.arrived + first_cta, 1);
-                last = before == last_cta - first_cta;
-                if (last) p.arrived[first_cta] = 0;
-            }
-            __syncthreads();
-            if (last) {
-                __threadfence();
-                for (int h = my_h; h < done_heads && c < p.dh; h += kRows) {
-                    float top = kNone, total = 0.0f;
-                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int a = first_cta; a <= last_cta; a += 4) {
-                        float t[4], l[4];
-                        float4 v[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int b = min(a + i, last_cta);
-                            const float* from = p.slots + (size_t)(2 * b + (b == first_cta ? 1 : 0)) * kSlotFloats;
-                            t[i] = a + i <= last_cta ? __ldcg(from + 16 * 256 + h) : kNone;
-                            l[i] = __ldcg(from + 16 * 256 + 16 + h);
-                            v[i] = __ldcg(reinterpret_cast<const float4*>(from + h * 256 + c));
-                        }
-                        const float higher = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), top);
-                        const float base = higher == kNone ? 0.0f : higher, keep = power2(top - base);
-                        top = higher;
-                        total *= keep;
-                        sum.x *= keep; sum.y *= keep; sum.z *= keep; sum.w *= keep;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float f = power2(t[i] - base);
-                            if (a + i > last_cta) continue;
-                            total = fmaf(f, l[i], total);
-                            sum.x = fmaf(f, v[i].x, sum.x); sum.y = fmaf(f, v[i].y, sum.y); sum.z = fmaf(f, v[i].z, sum.z); sum.w = fmaf(f, v[i].w, sum.w);
-                        }
-                    }
-                    write_result<T>(p, done.seq, done_head + h, c, sum, total);
-                    if (p.lse && c == 0) p.lse[(size_t)done.seq * p.q_heads + done_head + h] = (top == kNone ? 0.0f : top * kLn2) + logf(total);
-                }
-            }
+            const Cut cut = {first_cta, last_cta, done.seq, done_head, done_heads};
+            if (first_cta == cta) cuts[1] = cut;
+            else cuts[0] = cut;
         }
         if (!go) break;
         x += done.end - done.at;
+    }
+
+    // ---- heads that several CTAs share, the first and the last of this one's at most: who arrives last adds up, in the order of the CTAs ----
+    if (cuts[0].heads + cuts[1].heads == 0) return;
+    __threadfence();
+    __syncthreads();
+    if (tid < 2) {
+        const Cut c = tid ? cuts[1] : cuts[0];
+        bool mine = false;
+        if (c.heads > 0) {
+            mine = atomicAdd(p.arrived + c.first, 1) == c.last - c.first;
+            if (mine) p.arrived[c.first] = 0;
+        }
+        last[tid] = mine;
+    }
+    __syncthreads();
+    if (!last[0] && !last[1]) return;
+    __threadfence();
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        if (!last[k]) continue;
+        const Cut u = k ? cuts[1] : cuts[0];
+        // a row of threads takes a head, or where there are more rows than heads every so-manieth part of one
+        const int together = min(u.heads, kRows), groups = kRows / together, group = my_h / together;
+        for (int h0 = 0; h0 < u.heads; h0 += together) {
+            const int h = h0 + my_h % together;
+            const bool works = group < groups && h < u.heads && c < p.dh;
+            float top = kNone, total = 0.0f;
+            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (works) {
+                constexpr int kBatch = 8;
+                for (int a = u.first + group; a <= u.last; a += kBatch * groups) {
+                    float2 t[kBatch];
+                    float4 v[kBatch];
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int b = min(a + i * groups, u.last);
+                        const float* from = p.slots + (size_t)(2 * b + (b == u.first ? 1 : 0)) * kSlotFloats;
+                        t[i] = *reinterpret_cast<const float2*>(from + 16 * 256 + 2 * h);
+                        v[i] = *reinterpret_cast<const float4*>(from + h * 256 + c);
+                    }
+                    float higher = top;
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i)
+                        if (a + i * groups <= u.last) higher = fmaxf(higher, t[i].x);
+                    add_part(top, total, sum, higher, top, total, sum, true);
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i)
+                        if (a + i * groups <= u.last) add_part(top, total, sum, higher, t[i].x, t[i].y, v[i], false);
+                }
+            }
+            if (groups > 1) {                                 // (uniform)
+                float* const row = join + my_h * G::kJoinPitch;
+                __syncthreads();
+                if (works) {
+                    *reinterpret_cast<float4*>(row + c) = sum;
+                    if (c == 0) { row[G::kWidth] = top; row[G::kWidth + 1] = total; }
+                }
+                __syncthreads();
+                if (works && group == 0) {
+                    float higher = kNone;
+                    for (int g = 0; g < groups; ++g) higher = fmaxf(higher, join[(my_h + g * together) * G::kJoinPitch + G::kWidth]);
+                    top = kNone;
+                    for (int g = 0; g < groups; ++g) {
+                        const float* const other = join + (my_h + g * together) * G::kJoinPitch;
+                        add_part(top, total, sum, higher, other[G::kWidth], other[G::kWidth + 1], *reinterpret_cast<const float4*>(other + c), g == 0);
+                    }
+                }
+            }
+            if (works && group == 0) {
+                write_result<T>(p, u.seq, u.head + h, c, sum, total);
+                if (p.lse && c == 0) p.lse[(size_t)u.seq * p.q_heads + u.head + h] = (top == kNone ? 0.0f : top * kLn2) + logf(total);
+            }
+        }
     }
 }
 
