@@ -23,7 +23,7 @@ namespace {
 constexpr int kMaxCtas = 320;
 constexpr int kLeast = 4;                                     // tiles that a warp takes where heads are cut
 constexpr int kMaxParts = 64;                                 // a head's sums come from no more than about so many CTAs
-constexpr int kSlotFloats = 16 * 256 + 32;                    // sums of 16 heads, their maxima, their totals
+constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
 constexpr float kNone = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -37,6 +37,7 @@ struct AttendArgs {
     long long page_stride, token_stride, head_stride;         // bytes
     int ldq, ldo, q_heads, group, dh;
     int pages, page_size, page_shift, seqs, max_pages, table_ld, window;
+    int slot;                                                 // floats
     int kv_heads, heads_a_unit, units;                        // units: heads_a_unit query heads of one key-value head each, per sequence
     float scale, v_scale;                                     // scale: of the logits, the keys' scale included
 };
@@ -98,9 +99,16 @@ struct Walk {
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there)      // zeros where nothing is there; `src` is not read then
+// sixteen bytes, zeros where nothing is there (`src` is not read then); `once` marks the lines as the first to leave L2
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there, uint64_t once)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(once) : "memory");
+}
+__device__ __forceinline__ uint64_t read_once()
+{
+    uint64_t policy;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -698,6 +706,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     constexpr int kRowsACopy = 32 / G::kPieces ? 32 / G::kPieces : 1;                  // rows that one copy of the warp covers
     const int my_row = lane / G::kPieces, my_piece = lane % G::kPieces;
     const long long my_at = my_row * p.token_stride + 16 * my_piece;
+    const uint64_t once = read_once();
     auto copy_tile = [&](int stage) {                         // asks for the copies of the next tile and looks up the one after the one behind it
         const Pending t = near;
         near = far;
@@ -745,8 +754,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                     const int row = i * kRowsACopy + my_row;
                     const bool there = wanted && ((half >> row) & 1u);
                     const uint32_t to = dst + G::piece(16 * b + row, my_piece);
-                    copy16(to, there ? k : p.k, there);
-                    copy16(to + G::kHalf, there ? v : p.v, there);
+                    copy16(to, there ? k : p.k, there, once);
+                    copy16(to + G::kHalf, there ? v : p.v, there, once);
                     k += kRowsACopy * p.token_stride;
                     v += kRowsACopy * p.token_stride;
                 }
@@ -757,8 +766,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 const int idx = 32 * i + lane, row = idx / G::kPieces, c = idx % G::kPieces;
                 const long long from = __shfl_sync(0xffffffffu, at, row) + 16 * c;
                 const bool there = ((who >> row) & 1u) && 16 * c < p.dh * kBytes;
-                copy16(dst + G::piece(row, c), there ? t.keys + from : p.k, there);
-                copy16(dst + G::kHalf + G::piece(row, c), there ? t.values + from : p.v, there);
+                copy16(dst + G::piece(row, c), there ? t.keys + from : p.k, there, once);
+                copy16(dst + G::kHalf + G::piece(row, c), there ? t.values + from : p.v, there, once);
             }
         }
     };
@@ -801,11 +810,11 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const bool whole = done.end - done.at == n;
         const long long unit_at = x - (done.at - done.s.t0);
         const int first_cta = whole ? cta : (int)quotient(unit_at, share), last_cta = whole ? cta : (int)quotient(unit_at + n - 1, share);
-        float* slot = p.slots + (size_t)(2 * cta + (first_cta == cta ? 1 : 0)) * kSlotFloats;
+        float* slot = p.slots + (size_t)(2 * cta + (first_cta == cta ? 1 : 0)) * p.slot;
         if (tid < done_heads) {
             const float total = all.total(tid);
             if (!whole) {
-                *reinterpret_cast<float2*>(slot + 16 * 256 + 2 * tid) = make_float2(all.top(tid), total);
+                *reinterpret_cast<float2*>(slot + 2 * tid) = make_float2(all.top(tid), total);
             } else if (p.lse) {
                 p.lse[(size_t)done.seq * p.q_heads + done_head + tid] = all.base(tid) * kLn2 + logf(total);
             }
@@ -823,7 +832,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                     sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
                 }
                 if (whole) write_result<T>(p, done.seq, done_head + h0 + h, c, sum, all.total(h0 + h));
-                else *reinterpret_cast<float4*>(slot + (h0 + h) * 256 + c) = sum;
+                else *reinterpret_cast<float4*>(slot + 32 + (h0 + h) * p.dh + c) = sum;
             }
         }
         if (!whole) {
@@ -870,18 +879,19 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
 #pragma unroll
                     for (int i = 0; i < kBatch; ++i) {
                         const int b = min(a + i * groups, u.last);
-                        const float* from = p.slots + (size_t)(2 * b + (b == u.first ? 1 : 0)) * kSlotFloats;
-                        t[i] = *reinterpret_cast<const float2*>(from + 16 * 256 + 2 * h);
-                        v[i] = *reinterpret_cast<const float4*>(from + h * 256 + c);
+                        const float* from = p.slots + (size_t)(2 * b + (b == u.first ? 1 : 0)) * p.slot;
+                        t[i] = *reinterpret_cast<const float2*>(from + 2 * h);
+                        v[i] = *reinterpret_cast<const float4*>(from + 32 + h * p.dh + c);
                     }
                     float higher = top;
 #pragma unroll
-                    for (int i = 0; i < kBatch; ++i)
-                        if (a + i * groups <= u.last) higher = fmaxf(higher, t[i].x);
+                    for (int i = 0; i < kBatch; ++i) {
+                        if (a + i * groups > u.last) t[i] = make_float2(kNone, 0.0f);  // a part again: it weighs nothing (no branch, so that all loads fly at once)
+                        higher = fmaxf(higher, t[i].x);
+                    }
                     add_part(top, total, sum, higher, top, total, sum, true);
 #pragma unroll
-                    for (int i = 0; i < kBatch; ++i)
-                        if (a + i * groups <= u.last) add_part(top, total, sum, higher, t[i].x, t[i].y, v[i], false);
+                    for (int i = 0; i < kBatch; ++i) add_part(top, total, sum, higher, t[i].x, t[i].y, v[i], false);
                 }
             }
             if (groups > 1) {                                 // (uniform)
@@ -918,6 +928,7 @@ int launch_as(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
     const long long units = (long long)p.kv_heads * ceil_div(p.group, p.heads_a_unit);
     if (units > INT_MAX) return GELO_ERR_UNSUPPORTED;
     p.units = (int)units;
+    p.slot = 32 + p.heads_a_unit * p.dh;                      // a multiple of 8
     auto kernel = attend_kernel<T, W, kBytes>;
     GELO_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem));
     const int ctas = G::kCtas * ctx->sm_count < kMaxCtas ? G::kCtas * ctx->sm_count : kMaxCtas;
