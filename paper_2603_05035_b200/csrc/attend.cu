@@ -6,7 +6,8 @@
 // The work of a call is one line of tiles: sequence after sequence, key-value head after head, 16 or 32 positions a tile.  Every CTA works out
 // from the lengths which equal share of that line is its own, so ragged lengths balance and one long sequence fills the GPU.  What of
 // a (sequence, head) falls to one CTA is a segment; where a CTA's border cuts one, each side leaves its sums in the workspace and the
-// CTA that arrives last adds them up, in the order of the CTAs whoever that is.
+// CTA that arrives last adds them up, in the order of the CTAs whoever that is.  Where all sequences are short nothing is cut, and where there are
+// many heads besides, every warp takes heads of its own.
 // Inside a CTA the warps take the tiles of a segment in turn, each with a ring of its own in shared memory that asynchronous 16-byte copies
 // fill, so nothing but a segment's end makes them wait for one another.
 #include <limits.h>
@@ -22,6 +23,8 @@ namespace {
 
 constexpr int kMaxCtas = 320;
 constexpr int kLeast = 4;                                     // tiles that a warp takes where heads are cut
+constexpr int kWhole = 24;                                    // up to so many tiles a head stays in one piece
+constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
 constexpr int kMaxParts = 64;                                 // a head's sums come from no more than about so many CTAs
 constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
 constexpr float kNone = -INFINITY;
@@ -68,33 +71,88 @@ __device__ __forceinline__ Span span_of(const AttendArgs& p, int seq)
     return s;
 }
 
-// A walk over the segments of a CTA's share
+// A place in the line: tile `tile` (from its sequence's first) of (seq, unit)
+struct Place { int seq, unit, tile; };
+
+// A walk over the segments of a share
 template <int kTile>
 struct Walk {
     Span s;
     int seq, unit, at, end;                                   // the segment: tiles [at, end) of (seq, unit)
-    long long left;                                           // tiles of the share behind it
-    __device__ __forceinline__ void begin(const AttendArgs& p, int seq0, long long offset, long long tiles)
+    long long seq_at;                                         // where the sequence begins in the line
+    Place stop;
+    __device__ __forceinline__ bool last() const { return seq == stop.seq && unit == stop.unit; }
+    __device__ __forceinline__ void begin(const AttendArgs& p, const Place& from, long long from_at, const Place& to)
     {
-        seq = seq0;
+        seq = from.seq;
+        unit = from.unit;
+        seq_at = from_at;
+        stop = to;
         s = span_of<kTile>(p, seq);
-        const int n = s.t1 - s.t0;
-        unit = (int)quotient(offset, n);
-        at = s.t0 + (int)(offset - (long long)unit * n);
-        end = at + (int)min((long long)(s.t1 - at), tiles);
-        left = tiles - (end - at);
+        at = s.t0 + from.tile;
+        end = last() ? s.t0 + stop.tile : s.t1;
     }
-    __device__ __forceinline__ bool next(const AttendArgs& p)
+    __device__ __forceinline__ bool next(const AttendArgs& p, int cost)
     {
-        if (left <= 0) return false;
-        if (++unit == p.units) {
+        if (last()) return false;
+        const bool over = ++unit == p.units;
+        if (over) {
             unit = 0;
-            s = span_of<kTile>(p, ++seq);
+            seq_at += (long long)(s.t1 - s.t0 + cost) * p.units;
+            ++seq;
         }
+        if (last() && stop.tile == 0) return false;
+        if (over) s = span_of<kTile>(p, seq);
         at = s.t0;
-        end = at + (int)min((long long)(s.t1 - at), left);
-        left -= end - at;
+        end = last() ? s.t0 + stop.tile : s.t1;
         return true;
+    }
+};
+
+// The lengths of all sequences as a CTA's threads have added them up: thread i those of the sequences from i * per on
+template <int kWarps>
+struct Prefix {
+    long long inside[32 * kWarps];                            // tiles of a head before a thread's first sequence, of its warp's alone
+    long long warps[kWarps];                                  // tiles of a head of a warp's sequences
+    int longest[kWarps];
+    // The place at weight x of the line, in which a head of n tiles weighs n + cost; where nothing is cut, the first head that begins at x or behind.
+    // A warp works it out together; seq_at: the weight before the place's sequence.
+    template <int kTile>
+    __device__ __forceinline__ Place find(const AttendArgs& p, long long x, int per, int cost, bool whole, int lane, long long& seq_at) const
+    {
+        int i = -1;
+        long long before = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const int first = min((32 * w + lane) * per, p.seqs);
+            const long long at = (before + inside[32 * w + lane] + (long long)cost * first) * p.units;
+            i += __popc(__ballot_sync(0xffffffffu, first < p.seqs && at <= x));
+            before += warps[w];
+        }
+        before = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+            if (32 * (w + 1) <= i) before += warps[w];
+        Place at;
+        at.seq = i * per;
+        seq_at = (before + inside[i] + (long long)cost * at.seq) * p.units;
+        int n;
+        for (;;) {
+            const Span s = span_of<kTile>(p, at.seq);
+            n = s.t1 - s.t0 + cost;
+            if (x < seq_at + (long long)n * p.units || at.seq + 1 >= p.seqs) break;
+            seq_at += (long long)n * p.units;
+            ++at.seq;
+        }
+        at.unit = (int)quotient(x - seq_at, n);
+        const int offset = (int)(x - seq_at - (long long)at.unit * n);
+        at.tile = whole ? 0 : max(offset - cost, 0);
+        if (whole && offset > 0 && ++at.unit == p.units) {
+            at.unit = 0;
+            ++at.seq;
+            seq_at += (long long)n * p.units;
+        }
+        return at;
     }
 };
 
@@ -232,7 +290,7 @@ struct MmaWarp {
     float acc[DH / 16][NT][4];
     float m[NT][2], l[NT][2], scale[NT][2];
 
-    static constexpr int kStaged = 0;                         // floats of shared memory for q
+    static constexpr int kStaged = 0;                         // floats of shared memory for a warp's q
 
     // Asks for the q of a segment's heads; q points at the first one's components.  What arrives is taken up by begin().
     __device__ __forceinline__ void fetch(const AttendArgs& p, const T* q, int heads, int lane)
@@ -259,8 +317,7 @@ struct MmaWarp {
             }
         }
     }
-    __device__ __forceinline__ void stage(float*, int, int) {}
-    __device__ __forceinline__ void begin(const AttendArgs& p, const float*, int, int lane)
+    __device__ __forceinline__ void begin(const AttendArgs& p, float*, int lane)
     {
         const int t = lane & 3;
 #pragma unroll
@@ -438,8 +495,8 @@ struct MmaWarp {
                 }
             }
     }
-    // sums of heads [h0, h0 + kJoinHeads) brought to the maximum of all warps, head-major with the join's pitch
-    __device__ __forceinline__ void sums(float* out, const Joint<kHeads, G::kWarps>& all, int h0, int lane)
+    // sums of heads [h0, h0 + kJoinHeads) brought to the maximum of all warps (or as they are), head-major with the join's pitch
+    __device__ __forceinline__ void sums(float* out, const Joint<kHeads, G::kWarps>* all, int h0, int lane)
     {
         const int r = lane >> 2, t = lane & 3;
 #pragma unroll
@@ -448,7 +505,7 @@ struct MmaWarp {
             for (int j = 0; j < 2; ++j) {
                 const int h = 8 * n + 2 * t + j;
                 if (h < h0 || h >= h0 + G::kJoinHeads) continue;
-                const float f = power2(m[n][j] - all.base(h));
+                const float f = all ? power2(m[n][j] - all->base(h)) : 1.0f;
                 float* dst = out + (h - h0) * G::kJoinPitch;
 #pragma unroll
                 for (int s = 0; s < DH / 16; ++s) {
@@ -467,32 +524,27 @@ struct FmaWarp {
     using G = Tiles<DH, 4>;
     static constexpr int kHeads = H;
     static constexpr int kOwn = DH / 32;
-    static constexpr int kThreads = 32 * G::kWarps;
     static constexpr int kStaged = H * DH;
-    static constexpr int kMine = (kStaged + kThreads - 1) / kThreads;
+    static constexpr int kMine = kStaged / 32;
     const float* q;
     float held[kMine];
     float acc[H][kOwn];
     float m[H], l[H], scale;
 
-    __device__ __forceinline__ void fetch(const AttendArgs& p, const float* from, int heads, int)
+    __device__ __forceinline__ void fetch(const AttendArgs& p, const float* from, int heads, int lane)
     {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            const int at = i * kThreads + threadIdx.x, h = at / DH, c = at % DH;
+            const int at = 32 * i + lane, h = at / DH, c = at % DH;
             held[i] = h < heads && c < p.dh ? from[(size_t)h * p.dh + c] : 0.0f;
         }
     }
-    __device__ __forceinline__ void stage(float* staged, int, int)
+    __device__ __forceinline__ void begin(const AttendArgs& p, float* staged, int lane)
     {
+        __syncwarp();                                         // everybody is through with the last segment's
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int at = i * kThreads + threadIdx.x;
-            if (kStaged % kThreads == 0 || at < kStaged) staged[at] = held[i];
-        }
-    }
-    __device__ __forceinline__ void begin(const AttendArgs& p, const float* staged, int, int)
-    {
+        for (int i = 0; i < kMine; ++i) staged[32 * i + lane] = held[i];
+        __syncwarp();
         q = staged;
         scale = p.scale * kLog2e;
 #pragma unroll
@@ -576,12 +628,12 @@ struct FmaWarp {
             }
         }
     }
-    __device__ __forceinline__ void sums(float* out, const Joint<kHeads, G::kWarps>& all, int h0, int lane)
+    __device__ __forceinline__ void sums(float* out, const Joint<kHeads, G::kWarps>* all, int h0, int lane)
     {
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             if (h < h0 || h >= h0 + G::kJoinHeads) continue;
-            const float f = power2(m[h] - all.base(h));
+            const float f = all ? power2(m[h] - all->base(h)) : 1.0f;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) out[(h - h0) * G::kJoinPitch + component(lane, i)] = acc[h][i] * f;
         }
@@ -623,24 +675,24 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     using G = typename W::G;
     constexpr int kWarps = G::kWarps, kThreads = 32 * kWarps, kStages = G::kStages, kTile = G::kTile;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long scan[kWarps];
-    __shared__ long long found_offset;
-    __shared__ int found_seq, last[2];
+    __shared__ Prefix<kWarps> prefix;
+    __shared__ int last[2];
     __shared__ uint32_t counts[kWarps][kStages];
     __shared__ Joint<W::kHeads, kWarps> joint[2];             // of this segment, and of the one before or behind
-    __shared__ __align__(16) float staged[W::kStaged ? W::kStaged : 1];
+    __shared__ __align__(16) float staged[kWarps][W::kStaged ? W::kStaged : 1];
     chain_next();
     chain_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
 
-    // ---- this CTA's share of the line of tiles ----
-    long long x0, tiles, share;
+    // ---- this CTA's share of the line of tiles, or where `alone` this warp's ----
+    const int per = (p.seqs + kThreads - 1) / kThreads;
     {
-        const int per = (p.seqs + kThreads - 1) / kThreads, s0 = min(tid * per, p.seqs), s1 = min(s0 + per, p.seqs);
         long long mine = 0;
-        for (int s = s0; s < s1; ++s) {
+        int longest = 0;
+        for (int s = min(tid * per, p.seqs); s < min((tid + 1) * per, p.seqs); ++s) {
             const Span sp = span_of<kTile>(p, s);
             mine += sp.t1 - sp.t0;
+            longest = max(longest, sp.t1 - sp.t0);
         }
         long long upto = mine;
 #pragma unroll
@@ -648,44 +700,46 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             const long long u = __shfl_up_sync(0xffffffffu, upto, off);
             if (lane >= off) upto += u;
         }
-        if (lane == 31) scan[warp] = upto;
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        prefix.inside[tid] = upto - mine;
+        if (lane == 31) {
+            prefix.warps[warp] = upto;
+            prefix.longest[warp] = longest;
+        }
         __syncthreads();
-        long long all = 0;
+    }
+    long long all = 0;
+    int longest = 0;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) upto += scan[w];
-            all += scan[w];
-        }
-        const long long total = all * p.units;
-        // kLeast tiles for every warp, or a whole average head, since what a cut costs is more; and no head in many more than kMaxParts pieces
+    for (int w = 0; w < kWarps; ++w) {
+        all += prefix.warps[w];
+        longest = max(longest, prefix.longest[w]);
+    }
+    const bool whole = longest <= kWhole, alone = whole && (long long)p.seqs * p.units >= 2 * (long long)gridDim.x;
+    const int cost = alone ? kAloneCost : kSegmentCost, team = alone ? 1 : kWarps, member = alone ? 0 : warp;
+    const long long total = (all + (long long)cost * p.seqs) * p.units;
+    long long share = quotient(total + gridDim.x * (alone ? kWarps : 1) - 1, gridDim.x * (alone ? kWarps : 1));
+    if (!whole) {
+        // kLeast tiles for every warp, or an average head, since what a cut costs is more; and no head in many more than kMaxParts pieces
         const long long average = quotient(all + p.seqs - 1, p.seqs);
-        share = max(max(quotient(total + gridDim.x - 1, gridDim.x), min((long long)kLeast * kWarps, average)), (average + kMaxParts - 1) / kMaxParts);
-        x0 = cta * share;
-        tiles = min(share, total - x0);
-        if (tiles <= 0) return;
-        const long long before = (upto - mine) * p.units;
-        if (x0 >= before && x0 < upto * p.units) {
-            long long at = before;
-            int s = s0;
-            for (;;) {
-                const Span sp = span_of<kTile>(p, s);
-                const long long n = (long long)(sp.t1 - sp.t0) * p.units;
-                if (x0 < at + n || s + 1 >= s1) break;
-                at += n;
-                ++s;
-            }
-            found_seq = s;
-            found_offset = x0 - at;
-        }
-        __syncthreads();
+        share = max(share, max(min((long long)kLeast * kWarps, average), (average + kMaxParts - 1) / kMaxParts) + cost);
+    }
+    const long long x0 = (alone ? warp * (long long)gridDim.x + cta : cta) * share;
+    if (x0 >= total) return;                                  // (where not alone, all of the CTA; warps that are alone meet at no barrier)
+    Walk<kTile> ahead, walk;
+    {
+        long long from_at, to_at;
+        const Place from = prefix.template find<kTile>(p, x0, per, cost, whole, lane, from_at);
+        Place to = {p.seqs, 0, 0};
+        if (x0 + share < total) to = prefix.template find<kTile>(p, x0 + share, per, cost, whole, lane, to_at);
+        if (from.seq == to.seq && from.unit == to.unit && from.tile == to.tile) return;
+        ahead.begin(p, from, from_at, to);
+        walk = ahead;
     }
 
     // ---- copies: the tiles that this warp will take, in order, kStages - 1 of them ahead ----
     const uint32_t ring = smem_at(smem) + warp * kStages * G::kStage;
     float* const join = reinterpret_cast<float*>(smem + kWarps * kStages * G::kStage);
-    Walk<kTile> ahead, walk;
-    ahead.begin(p, found_seq, found_offset, tiles);
-    walk = ahead;
     W w;
     int first_head, heads;                                    // of the segment
     auto fetch = [&](const Walk<kTile>& at) {
@@ -695,7 +749,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         w.fetch(p, static_cast<const T*>(p.q) + (size_t)at.seq * p.ldq + (size_t)first_head * p.dh, heads, lane);
     };
     fetch(walk);
-    int next_tile = ahead.at + warp;
+    int next_tile = ahead.at + member;
     bool more = true;
     // The next two tiles whose copies have not been asked for: the page that each position (lane % kTile) is on is looked up that far ahead.
     struct Pending {
@@ -711,8 +765,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const Pending t = near;
         near = far;
         while (more && next_tile >= ahead.end) {
-            more = ahead.next(p);
-            next_tile = ahead.at + warp;
+            more = ahead.next(p, cost);
+            next_tile = ahead.at + member;
         }
         far.any = more;
         far.on = false;
@@ -727,7 +781,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             const long long head_at = (ahead.unit / (p.units / p.kv_heads)) * p.head_stride;
             far.keys = static_cast<const char*>(p.k) + head_at;
             far.values = static_cast<const char*>(p.v) + head_at;
-            next_tile += kWarps;
+            next_tile += team;
         }
         if (!t.any) return;
         __syncwarp();                                         // everybody has read what the stage held
@@ -773,16 +827,13 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     };
 
     // ---- segments ----
-    w.stage(staged, tid, lane);
-    if constexpr (W::kStaged > 0) __syncthreads();
     Cut cuts[2] = {};
     constexpr int kQuads = G::kWidth / 4, kRows = kThreads / kQuads;                          // a row of threads adds up a head, four components each
     const int c = 4 * (tid % kQuads), my_h = tid / kQuads;
     int put = 0, get = 0, turn = 0, lead = -2;                // lead: tiles asked for and not used (the first two rounds only look up)
-    long long x = x0;                                         // where the segment begins
     for (;; turn ^= 1) {
-        w.begin(p, staged, tid, lane);
-        for (int t = walk.at + warp; t < walk.end; t += kWarps) {
+        w.begin(p, staged[warp], lane);
+        for (int t = walk.at + member; t < walk.end; t += team) {
 #pragma unroll 1
             for (; lead < kStages; ++lead) {
                 copy_tile(put);
@@ -802,18 +853,38 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         w.statistics(all.tops[warp], all.totals[warp], lane);
         const Walk<kTile> done = walk;
         const int done_head = first_head, done_heads = heads;
-        const bool go = walk.next(p);
+        const bool go = walk.next(p, cost);
         if (go) fetch(walk);
+        if (alone) {
+            float* const mine = join + warp * G::kJoinHeads * G::kJoinPitch;
+            __syncwarp();
+            if (p.lse && lane < done_heads) {
+                const float top = all.tops[warp][lane];
+                p.lse[(size_t)done.seq * p.q_heads + done_head + lane] = (top == kNone ? 0.0f : top * kLn2) + logf(all.totals[warp][lane]);
+            }
+            for (int h0 = 0; h0 < done_heads; h0 += G::kJoinHeads) {
+                __syncwarp();
+                w.sums(mine, nullptr, h0, lane);
+                __syncwarp();
+                for (int i = lane; i < min(done_heads - h0, G::kJoinHeads) * kQuads; i += 32) {
+                    const int h = i / kQuads, at = 4 * (i % kQuads);
+                    if (at < p.dh)
+                        write_result<T>(p, done.seq, done_head + h0 + h, at, *reinterpret_cast<const float4*>(mine + h * G::kJoinPitch + at), all.totals[warp][h0 + h]);
+                }
+            }
+            __syncwarp();
+            if (!go) return;
+            continue;
+        }
         __syncthreads();
-        if (go) w.stage(staged, tid, lane);
         const int n = done.s.t1 - done.s.t0;
-        const bool whole = done.end - done.at == n;
-        const long long unit_at = x - (done.at - done.s.t0);
-        const int first_cta = whole ? cta : (int)quotient(unit_at, share), last_cta = whole ? cta : (int)quotient(unit_at + n - 1, share);
+        const bool in_one = done.end - done.at == n;
+        const long long unit_at = done.seq_at + (long long)done.unit * (n + cost) + cost;
+        const int first_cta = in_one ? cta : (int)quotient(unit_at, share), last_cta = in_one ? cta : (int)quotient(unit_at + n - 1, share);
         float* slot = p.slots + (size_t)(2 * cta + (first_cta == cta ? 1 : 0)) * p.slot;
         if (tid < done_heads) {
             const float total = all.total(tid);
-            if (!whole) {
+            if (!in_one) {
                 *reinterpret_cast<float2*>(slot + 2 * tid) = make_float2(all.top(tid), total);
             } else if (p.lse) {
                 p.lse[(size_t)done.seq * p.q_heads + done_head + tid] = all.base(tid) * kLn2 + logf(total);
@@ -821,7 +892,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         }
         for (int h0 = 0; h0 < done_heads; h0 += G::kJoinHeads) {
             if (h0 > 0) __syncthreads();
-            w.sums(join + warp * G::kJoinHeads * G::kJoinPitch, all, h0, lane);
+            w.sums(join + warp * G::kJoinHeads * G::kJoinPitch, &all, h0, lane);
             __syncthreads();
             const int some = min(done_heads - h0, G::kJoinHeads);
             for (int h = my_h; h < some && c < p.dh; h += kRows) {
@@ -831,17 +902,16 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                     const float4 v = *reinterpret_cast<const float4*>(join + (j * G::kJoinHeads + h) * G::kJoinPitch + c);
                     sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
                 }
-                if (whole) write_result<T>(p, done.seq, done_head + h0 + h, c, sum, all.total(h0 + h));
+                if (in_one) write_result<T>(p, done.seq, done_head + h0 + h, c, sum, all.total(h0 + h));
                 else *reinterpret_cast<float4*>(slot + 32 + (h0 + h) * p.dh + c) = sum;
             }
         }
-        if (!whole) {
+        if (!in_one) {
             const Cut cut = {first_cta, last_cta, done.seq, done_head, done_heads};
             if (first_cta == cta) cuts[1] = cut;
             else cuts[0] = cut;
         }
         if (!go) break;
-        x += done.end - done.at;
     }
 
     // ---- heads that several CTAs share, the first and the last of this one's at most: who arrives last adds up, in the order of the CTAs ----
@@ -955,7 +1025,7 @@ int launch_fma(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
 {
     if (p.dh <= 64) return launch_as<float, FmaWarp<64, H>, 4>(ctx, p, st);
     if (p.dh <= 128) return launch_as<float, FmaWarp<128, H>, 4>(ctx, p, st);
-    return launch_as<float, FmaWarp<256, H>, 4>(ctx, p, st);
+    return launch_as<float, FmaWarp<256, H < 4 ? H : 4>, 4>(ctx, p, st);             // (eight would not leave room for their sums in registers)
 }
 
 }  // namespace
