@@ -115,6 +115,16 @@ def load_library():
     return _lib
 
 
+_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _code_of(t) -> int:
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"unsupported dtype {t.dtype!r}")
+    return code
+
+
 def dtype_code(dtype) -> int:
     if dtype in (F32, "f32", torch.float32):
         return F32
@@ -135,9 +145,14 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _current_stream(device: int) -> int:
+    """Handle of torch's current stream on a device (without the Stream object that torch.cuda.current_stream builds, 3 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -186,6 +201,7 @@ class PagedCache:
             raise ValueError("the rows of table must be contiguous and apart")
         self.k, self.v, self.table, self.dtype, self.device = k, v, table, code, k.device
         self.pages, self.page_size, self.kv_heads, self.head_dim = k.shape
+        self.index, self.default_scale = k.get_device(), self.head_dim ** -0.5
         self.seqs = table.shape[0]
         # the stride of a dimension of one entry is never used; torch reports any value for it
         strides = [self.head_dim if k.shape[i] <= 1 else k.stride(i) for i in range(3)]
@@ -373,32 +389,34 @@ class Context:
     # ---- around the projection -------------------------------------------------------------
     def _rows(self, t, name, dtype, rows, width):
         """Pointer and row stride of a matrix whose rows are contiguous."""
-        if t.device.index != self.device or not t.is_cuda:
-            raise ValueError(f"{name} is on {t.device}, the context on cuda:{self.device}")
-        if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
-            raise ValueError(f"{name} must be {rows} x {width} of {dtype}, not {tuple(t.shape)} of {t.dtype}")
-        if t.stride(1) != 1 and width > 1:
+        if t.dtype is not dtype or t.shape != (rows, width) or t.get_device() != self.device:
+            raise ValueError(f"{name} must be {rows} x {width} of {dtype} on cuda:{self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        ld, one = t.stride()
+        if one != 1 and width > 1:
             raise ValueError(f"the rows of {name} must be contiguous")
-        ld = t.stride(0) if rows > 1 else (width + 15) // 16 * 16      # (the stride of a single row is never used)
-        if ld >= 1 << 31:
+        if rows <= 1:
+            ld = (width + 15) // 16 * 16                         # (never used)
+        elif ld >= 1 << 31:
             raise ValueError(f"the rows of {name} are too far apart")
         return t.data_ptr(), ld
 
     def _vector(self, t, name, dtype, count):
-        if t.device.index != self.device or not t.is_cuda:
-            raise ValueError(f"{name} is on {t.device}, the context on cuda:{self.device}")
-        if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
-            raise ValueError(f"{name} must hold {count} contiguous values of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+        if t.dtype is not dtype or t.numel() != count or t.get_device() != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} must hold {count} contiguous values of {dtype} on cuda:{self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         return t.data_ptr()
 
     def _on(self, stream):
-        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else _stream(stream)
+        return _current_stream(self.device) if stream is None else _stream(stream)
+
+    def _here(self, cache):
+        if cache.index != self.device:
+            raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
 
     def rms_norm(self, X, Y=None, weight=None, eps=1e-5, residual=None, residual_out=None, codes=None, row_scale=None, stream=None):
         """Y = rms-normalised X + residual, times weight; residual_out = X + residual; codes and row_scale: the result in E4M3 (uint8 or
         float8_e4m3fn) with a scale per row.  X: rows x d, rows may be strided; the type is X's."""
         rows, d = X.shape
-        dt = X.dtype
+        dt, code = X.dtype, _code_of(X)
         x, ldx = self._rows(X, "X", dt, rows, d)
         y, ldy = self._rows(Y, "Y", dt, rows, d) if Y is not None else (None, 0)
         r, ldr = self._rows(residual, "residual", dt, rows, d) if residual is not None else (None, 0)
@@ -406,7 +424,7 @@ class Context:
         c, ldc = (None, 0) if codes is None else self._rows(codes, "codes", codes.dtype if codes.element_size() == 1 else torch.uint8, rows, d)
         s = self._vector(row_scale, "row_scale", torch.float32, rows) if row_scale is not None else None
         w = self._vector(weight, "weight", dt, d) if weight is not None else None
-        self._check(self._lib.gelo_rms_norm(self._h, x, ldx, r, ldr, w, rows, d, eps, dtype_code(dt), ro, ldro, y, ldy, c, ldc, s,
+        self._check(self._lib.gelo_rms_norm(self._h, x, ldx, r, ldr, w, rows, d, eps, code, ro, ldro, y, ldy, c, ldc, s,
                                             self._on(stream)), "gelo_rms_norm")
 
     def rope_turns(self, turns, base=10000.0, factor=1.0, original=0.0, low=1.0, high=32.0, stream=None):
@@ -418,21 +436,21 @@ class Context:
     def rotary(self, X, heads, pos, rope, Y=None, stream=None):
         """Y (default: X itself) = X, n rows of `heads` heads, rotated to the positions pos (int32)."""
         n, width = X.shape
+        code = _code_of(X)
         Y = X if Y is None else Y
         if heads < 1 or width % heads:
             raise ValueError("the width of X must be a multiple of heads")
         x, ldx = self._rows(X, "X", X.dtype, n, width)
         y, ldy = self._rows(Y, "Y", X.dtype, n, width)
         self._check(self._lib.gelo_rotary(self._h, x, ldx, n, heads, width // heads, self._vector(pos, "pos", torch.int32, n), rope.ref,
-                                          dtype_code(X.dtype), y, ldy, self._on(stream)), "gelo_rotary")
+                                          code, y, ldy, self._on(stream)), "gelo_rotary")
 
     def append_kv(self, cache, K, V, pos, seq=None, rope=None, Q=None, Q_out=None, stream=None):
         """K (rotated) and V, n rows of kv_heads heads, go to position pos[i] of sequence seq[i] (default i); Q rotated goes to Q_out
         (default: Q itself)."""
         n, width = K.shape[0], cache.kv_heads * cache.head_dim
-        dt = K.dtype
-        if cache.device.index != self.device:
-            raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
+        dt, code = K.dtype, _code_of(K)
+        self._here(cache)
         k, ldk = self._rows(K, "K", dt, n, width)
         v, ldv = self._rows(V, "V", dt, n, width)
         q, ldq, qo, ldqo, heads = None, 0, None, 0, 0
@@ -446,7 +464,7 @@ class Context:
             raise ValueError("Q_out without Q")
         s = self._vector(seq, "seq", torch.int32, n) if seq is not None else None
         self._check(self._lib.gelo_append_kv(self._h, cache.ref, k, ldk, v, ldv, q, ldq, heads, n, s, self._vector(pos, "pos", torch.int32, n),
-                                             rope.ref if rope is not None else None, dtype_code(dt), qo, ldqo, self._on(stream)),
+                                             rope.ref if rope is not None else None, code, qo, ldqo, self._on(stream)),
                     "gelo_append_kv")
 
     def ensure_attention_workspace(self):
@@ -459,18 +477,17 @@ class Context:
     def paged_attention(self, cache, Q, lengths, O, scale=None, window=0, lse=None, stream=None):
         """O = attention of one new token per sequence (row s of Q: q_heads heads) over the first lengths[s] positions of the cache, or the last
         `window` of them; scale defaults to head_dim^-1/2; lse (sequences x q_heads, fp32) receives the logarithm of the softmax's sum."""
-        if cache.device.index != self.device:
-            raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
+        self._here(cache)
         heads, rest = divmod(Q.shape[1], cache.head_dim)
         if rest:
             raise ValueError("the width of Q must be a multiple of head_dim")
-        dt = Q.dtype
+        dt, code = Q.dtype, _code_of(Q)
         q, ldq = self._rows(Q, "Q", dt, cache.seqs, Q.shape[1])
         o, ldo = self._rows(O, "O", dt, cache.seqs, Q.shape[1])
         ln = self._vector(lengths, "lengths", torch.int32, cache.seqs)
         ls = self._vector(lse, "lse", torch.float32, cache.seqs * heads) if lse is not None else None
-        self._check(self._lib.gelo_paged_attention(self._h, cache.ref, q, ldq, heads, ln, cache.head_dim ** -0.5 if scale is None else scale,
-                                                   window, dtype_code(dt), o, ldo, ls, self._on(stream)), "gelo_paged_attention")
+        self._check(self._lib.gelo_paged_attention(self._h, cache.ref, q, ldq, heads, ln, cache.default_scale if scale is None else scale,
+                                                   window, code, o, ldo, ls, self._on(stream)), "gelo_paged_attention")
 
     def unmix(self, Ainv, lda, Yp, n, k, p, dtype, Q, K=None, V=None, stream=None):
         self._check(self._lib.gelo_unmix(self._h, _ptr(Ainv), lda, _ptr(Yp), n, k, p, dtype_code(dtype),

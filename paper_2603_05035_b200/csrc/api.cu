@@ -198,12 +198,13 @@ int check_cache(const gelo_kv_cache* c, int dtype)
 
 struct DeviceGuard {
     int prev = -1;
-    bool ok = true;
+    bool ok = true, moved = false;
     explicit DeviceGuard(int dev) {
         if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+        moved = prev != dev;
+        if (moved && cudaSetDevice(dev) != cudaSuccess) ok = false;
     }
-    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+    ~DeviceGuard() { if (moved) cudaSetDevice(prev); }
 };
 
 __global__ void set_scalar_kernel(float* p, float v) { *p = v; }

@@ -12,6 +12,7 @@
 // fill, so nothing but a segment's end makes them wait for one another.
 #include <limits.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "common.cuh"
@@ -1000,7 +1001,13 @@ int launch_as(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
     p.units = (int)units;
     p.slot = 32 + p.heads_a_unit * p.dh;                      // a multiple of 8
     auto kernel = attend_kernel<T, W, kBytes>;
-    GELO_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem));
+    // once per device: the attribute stays (asking again costs the host a microsecond)
+    static std::atomic<uint64_t> allowed{0};
+    const uint64_t bit = ctx->device < 64 ? 1ull << ctx->device : 0;
+    if (!(allowed.load(std::memory_order_acquire) & bit)) {
+        GELO_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmem));
+        allowed.fetch_or(bit, std::memory_order_release);
+    }
     const int ctas = G::kCtas * ctx->sm_count < kMaxCtas ? G::kCtas * ctx->sm_count : kMaxCtas;
     GELO_TRY(launch_chained(ctx, kernel, dim3(ctas), 32 * G::kWarps, G::kSmem, st, p));
     return after_launch(ctx);
