@@ -1479,7 +1479,9 @@ int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda
     if ((lda % 16) || (ldb % 16) || (ldc % 8) || (N % 8) || !aligned16(A8) || !aligned16(B8) || !aligned16(C) || !sa || !sb)
         return GELO_ERR_INVALID;
     EncodeTiledFn enc = reinterpret_cast<EncodeTiledFn>(ctx->tmap_encode);
-    const bool pair = use_pair(ctx, M, N, 1, false, TC_STORE_BF16);
+    // narrow tiles while they still find an SM each: W is then streamed by twice as many SMs (64 rows, K = 4096, N = 12288)
+    const bool narrow = ceil_div(M, BM) * ceil_div(N, 128) <= ctx->sm_count;
+    const bool pair = !narrow && use_pair(ctx, M, N, 1, false, TC_STORE_BF16);
     CUtensorMap ma, mb;
     {
         const cuuint64_t dims[2] = { (cuuint64_t)K, (cuuint64_t)M };
@@ -1491,7 +1493,7 @@ int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda
             return GELO_ERR_CUDA;
     }
     bool b3d = false;
-    if (!make_map_nmajor(ctx, &mb, B8, 1, false, (uint64_t)N, (uint64_t)K, (uint64_t)ldb, 128, pair ? 128 : 256, &b3d)) return GELO_ERR_CUDA;
+    if (!make_map_nmajor(ctx, &mb, B8, 1, false, (uint64_t)N, (uint64_t)K, (uint64_t)ldb, 128, pair || narrow ? 128 : 256, &b3d)) return GELO_ERR_CUDA;
     TcParams p = {};
     p.M = M; p.N = N;
     p.nseg = 1;
@@ -1504,6 +1506,7 @@ int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda
     p.scale_a = sa; p.scale_b = sb;
     p.scale_a_step = sa_rows ? 1 : 0;
     p.status = ctx->status_dev;
+    if (narrow) return launch_tiles<128, false, false, false, true>(ctx, false, ma, ma, mb, mb, ma, p, 2.0 * M * (double)N * K, st);
     return launch_tiles<256, false, false, false, true>(ctx, pair, ma, ma, mb, mb, ma, p, 2.0 * M * (double)N * K, st);
 }
 

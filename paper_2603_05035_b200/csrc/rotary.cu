@@ -2,7 +2,7 @@
 //   x_a' = (x_a cos - x_b sin) m,  x_b' = (x_b cos + x_a sin) m,   angle = 2 pi position turns[pair]
 // A CTA takes one token: its threads first work out the cosines and sines of all pairs, which all heads share, then stream the heads
 // of Q, K and V through.  position * turns is formed and reduced to one circle in binary64 (a position times an fp32 frequency is off
-// by position * 2^-24), the rest is fp32.  Every pair belongs to one thread, which reads both values before it writes either, so Q may be
+// by position * 2^-24), and so are the cosine and sine, which are then rounded once; the rest is fp32.  Every pair belongs to one thread, which reads both values before it writes either, so Q may be
 // rotated in place.  Bound by HBM: Q, K and V in, all three out.
 #include "common.cuh"
 #include "vec8.cuh"
@@ -49,6 +49,13 @@ __device__ __forceinline__ void put1(uint8_t* dst, float v, float scale)
     *dst = (uint8_t)__nv_cvt_float_to_fp8(__fdiv_rn(v, scale), __NV_SATFINITE, __NV_E4M3);
 }
 
+// Both components of a pair; products and sum rounded one by one, so that they do not depend on what the compiler fuses
+__device__ __forceinline__ void rotate(float u, float w, float2 cs, float& x, float& y)
+{
+    x = __fsub_rn(__fmul_rn(u, cs.x), __fmul_rn(w, cs.y));
+    y = __fadd_rn(__fmul_rn(w, cs.x), __fmul_rn(u, cs.y));
+}
+
 // One piece of a head: kWide pieces are eight components, or eight pairs in the half layout; else one component or pair.
 template <typename T, typename C, bool kWide>
 __device__ __forceinline__ void rotate_piece(const T* src, C* dst, int piece, const RotateArgs& p, const float2* turn, float scale)
@@ -66,8 +73,7 @@ __device__ __forceinline__ void rotate_piece(const T* src, C* dst, int piece, co
                 if (c0 + j < p.rot) {
                     const float2 cs = turn[(c0 + j) >> 1];
                     const float u = a[j], w = a[j + 1];
-                    a[j] = u * cs.x - w * cs.y;
-                    a[j + 1] = w * cs.x + u * cs.y;
+                    rotate(u, w, cs, a[j], a[j + 1]);
                 }
             }
             put8(dst + c0, a, scale);
@@ -81,8 +87,7 @@ __device__ __forceinline__ void rotate_piece(const T* src, C* dst, int piece, co
             for (int j = 0; j < 8; ++j) {
                 const float2 cs = turn[c0 + j];
                 const float u = a[j], w = b[j];
-                a[j] = u * cs.x - w * cs.y;
-                b[j] = w * cs.x + u * cs.y;
+                rotate(u, w, cs, a[j], b[j]);
             }
             put8(dst + c0, a, scale);
             put8(dst + c0 + half, b, scale);
@@ -96,8 +101,10 @@ __device__ __forceinline__ void rotate_piece(const T* src, C* dst, int piece, co
         if (piece < half) {
             const float2 cs = turn[piece];
             const float u = widen_at(src, piece), w = widen_at(src, piece + half);
-            put1(dst + piece, u * cs.x - w * cs.y, scale);
-            put1(dst + piece + half, w * cs.x + u * cs.y, scale);
+            float x, y;
+            rotate(u, w, cs, x, y);
+            put1(dst + piece, x, scale);
+            put1(dst + piece + half, y, scale);
         } else {
             put1(dst + piece + half, widen_at(src, piece + half), scale);
         }
@@ -116,11 +123,10 @@ __global__ void __launch_bounds__(kThreads) rotate_append_kernel(const RotateArg
     if (pos < 0) return;
     const int half = p.rot >> 1;
     for (int i = threadIdx.x; i < half; i += kThreads) {
-        double t = (double)pos * p.turns[i];
+        double t = (double)pos * p.turns[i], s, c;
         t -= rint(t);
-        float s, c;
-        sincospif((float)(2.0 * t), &s, &c);
-        turn[i] = make_float2(c * p.magnitude, s * p.magnitude);
+        sincospi(2.0 * t, &s, &c);
+        turn[i] = make_float2((float)c * p.magnitude, (float)s * p.magnitude);
     }
     long long at = -1;                                        // the token's place in the cache
     if (p.k) {
