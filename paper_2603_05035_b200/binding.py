@@ -1,7 +1,8 @@
 """ctypes binding of ``libgelo.so`` -- argument marshalling only.
 
 Every function here has the name and the arguments of the C entry point declared in
-``include/gelo.h``; tensors are torch CUDA tensors whose ``data_ptr()`` is handed over.
+``include/gelo.h``; tensors are torch CUDA tensors whose ``data_ptr()`` is handed over.  The calls around the
+projection, which a decode step makes one by one, go through ``_marshal.so`` (``csrc/marshal.cpp``) instead of ctypes.
 All arithmetic of the path runs in the library's kernels.  A missing library is an
 error: there is no other implementation to fall back to.
 """
@@ -15,6 +16,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libgelo.so")
 _lib = None
+_marshal = None
 
 OK, ERR_INVALID, ERR_WORKSPACE, ERR_COND, ERR_TIMEOUT, ERR_CUDA, ERR_UNSUPPORTED = range(7)
 ORTHOGONAL, NONORTHOGONAL = 0, 1
@@ -101,28 +103,19 @@ def library_path() -> str:
 
 def load_library():
     """Loads the CUDA library; raises if it has not been built (no fallback exists)."""
-    global _lib
+    global _lib, _marshal
     if _lib is None:
-        if not os.path.exists(_LIB_PATH):
-            raise FileNotFoundError(
-                f"{_LIB_PATH} is missing: build it with `python -m paper_2603_05035_b200.build`")
+        for path in (_LIB_PATH, os.path.join(_HERE, "_marshal.so")):
+            if not os.path.exists(path):
+                raise FileNotFoundError(f"{path} is missing: build it with `python -m paper_2603_05035_b200.build`")
         lib = ctypes.CDLL(_LIB_PATH)
         for name, (res, args) in EXPORTS.items():
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args
-        _lib = lib
+        from . import _marshal as m                              # (finds libgelo.so beside it, already loaded)
+        _lib, _marshal = lib, m
     return _lib
-
-
-_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-
-
-def _code_of(t) -> int:
-    code = _CODES.get(t.dtype)
-    if code is None:
-        raise ValueError(f"unsupported dtype {t.dtype!r}")
-    return code
 
 
 def dtype_code(dtype) -> int:
@@ -224,12 +217,13 @@ class Context:
         h = _vp()
         self._check(self._lib.gelo_create(ctypes.byref(h), self.device), "gelo_create")
         self._h = h
+        self._handle = h.value
         self._ws = None
 
     def close(self):
         if getattr(self, "_h", None):
             self._lib.gelo_destroy(self._h)
-            self._h = None
+            self._h = self._handle = None
 
     def __del__(self):  # pragma: no cover
         try:
@@ -387,27 +381,6 @@ class Context:
                                                      _stream(stream)), "gelo_project_e4m3_rows")
 
     # ---- around the projection -------------------------------------------------------------
-    def _rows(self, t, name, dtype, rows, width):
-        """Pointer and row stride of a matrix whose rows are contiguous."""
-        if t.dtype is not dtype or t.shape != (rows, width) or t.get_device() != self.device:
-            raise ValueError(f"{name} must be {rows} x {width} of {dtype} on cuda:{self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-        ld, one = t.stride()
-        if one != 1 and width > 1:
-            raise ValueError(f"the rows of {name} must be contiguous")
-        if rows <= 1:
-            ld = (width + 15) // 16 * 16                         # (never used)
-        elif ld >= 1 << 31:
-            raise ValueError(f"the rows of {name} are too far apart")
-        return t.data_ptr(), ld
-
-    def _vector(self, t, name, dtype, count):
-        if t.dtype is not dtype or t.numel() != count or t.get_device() != self.device or not t.is_contiguous():
-            raise ValueError(f"{name} must hold {count} contiguous values of {dtype} on cuda:{self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-        return t.data_ptr()
-
-    def _on(self, stream):
-        return _current_stream(self.device) if stream is None else _stream(stream)
-
     def _here(self, cache):
         if cache.index != self.device:
             raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
@@ -415,56 +388,25 @@ class Context:
     def rms_norm(self, X, Y=None, weight=None, eps=1e-5, residual=None, residual_out=None, codes=None, row_scale=None, stream=None):
         """Y = rms-normalised X + residual, times weight; residual_out = X + residual; codes and row_scale: the result in E4M3 (uint8 or
         float8_e4m3fn) with a scale per row.  X: rows x d, rows may be strided; the type is X's."""
-        rows, d = X.shape
-        dt, code = X.dtype, _code_of(X)
-        x, ldx = self._rows(X, "X", dt, rows, d)
-        y, ldy = self._rows(Y, "Y", dt, rows, d) if Y is not None else (None, 0)
-        r, ldr = self._rows(residual, "residual", dt, rows, d) if residual is not None else (None, 0)
-        ro, ldro = self._rows(residual_out, "residual_out", dt, rows, d) if residual_out is not None else (None, 0)
-        c, ldc = (None, 0) if codes is None else self._rows(codes, "codes", codes.dtype if codes.element_size() == 1 else torch.uint8, rows, d)
-        s = self._vector(row_scale, "row_scale", torch.float32, rows) if row_scale is not None else None
-        w = self._vector(weight, "weight", dt, d) if weight is not None else None
-        self._check(self._lib.gelo_rms_norm(self._h, x, ldx, r, ldr, w, rows, d, eps, code, ro, ldro, y, ldy, c, ldc, s,
-                                            self._on(stream)), "gelo_rms_norm")
+        self._check(_marshal.rms_norm(self._handle, self.device, X, Y, weight, eps, residual, residual_out, codes, row_scale, stream), "gelo_rms_norm")
 
     def rope_turns(self, turns, base=10000.0, factor=1.0, original=0.0, low=1.0, high=32.0, stream=None):
         """Fills turns (float64, rot / 2 values): turns per position of each pair, stretched for long contexts."""
-        t = self._vector(turns, "turns", torch.float64, turns.numel())
-        self._check(self._lib.gelo_rope_turns(self._h, 2 * turns.numel(), base, factor, original, low, high, t, self._on(stream)),
-                    "gelo_rope_turns")
+        _want(turns, "turns", torch.float64, 1)
+        if turns.get_device() != self.device or not turns.is_contiguous():
+            raise ValueError(f"turns must be contiguous and on cuda:{self.device}")
+        self._check(self._lib.gelo_rope_turns(self._h, 2 * turns.numel(), base, factor, original, low, high, turns.data_ptr(),
+                                              _current_stream(self.device) if stream is None else _stream(stream)), "gelo_rope_turns")
 
     def rotary(self, X, heads, pos, rope, Y=None, stream=None):
         """Y (default: X itself) = X, n rows of `heads` heads, rotated to the positions pos (int32)."""
-        n, width = X.shape
-        code = _code_of(X)
-        Y = X if Y is None else Y
-        if heads < 1 or width % heads:
-            raise ValueError("the width of X must be a multiple of heads")
-        x, ldx = self._rows(X, "X", X.dtype, n, width)
-        y, ldy = self._rows(Y, "Y", X.dtype, n, width)
-        self._check(self._lib.gelo_rotary(self._h, x, ldx, n, heads, width // heads, self._vector(pos, "pos", torch.int32, n), rope.ref,
-                                          code, y, ldy, self._on(stream)), "gelo_rotary")
+        self._check(_marshal.rotary(self._handle, self.device, X, heads, pos, rope.ref, Y, stream), "gelo_rotary")
 
     def append_kv(self, cache, K, V, pos, seq=None, rope=None, Q=None, Q_out=None, stream=None):
         """K (rotated) and V, n rows of kv_heads heads, go to position pos[i] of sequence seq[i] (default i); Q rotated goes to Q_out
         (default: Q itself)."""
-        n, width = K.shape[0], cache.kv_heads * cache.head_dim
-        dt, code = K.dtype, _code_of(K)
         self._here(cache)
-        k, ldk = self._rows(K, "K", dt, n, width)
-        v, ldv = self._rows(V, "V", dt, n, width)
-        q, ldq, qo, ldqo, heads = None, 0, None, 0, 0
-        if Q is not None:
-            heads, rest = divmod(Q.shape[1], cache.head_dim)
-            if rest:
-                raise ValueError("the width of Q must be a multiple of head_dim")
-            q, ldq = self._rows(Q, "Q", dt, n, Q.shape[1])
-            qo, ldqo = (q, ldq) if Q_out is None else self._rows(Q_out, "Q_out", dt, n, Q.shape[1])
-        elif Q_out is not None:
-            raise ValueError("Q_out without Q")
-        s = self._vector(seq, "seq", torch.int32, n) if seq is not None else None
-        self._check(self._lib.gelo_append_kv(self._h, cache.ref, k, ldk, v, ldv, q, ldq, heads, n, s, self._vector(pos, "pos", torch.int32, n),
-                                             rope.ref if rope is not None else None, code, qo, ldqo, self._on(stream)),
+        self._check(_marshal.append_kv(self._handle, self.device, cache.ref, K, V, pos, seq, None if rope is None else rope.ref, Q, Q_out, stream),
                     "gelo_append_kv")
 
     def ensure_attention_workspace(self):
@@ -478,16 +420,8 @@ class Context:
         """O = attention of one new token per sequence (row s of Q: q_heads heads) over the first lengths[s] positions of the cache, or the last
         `window` of them; scale defaults to head_dim^-1/2; lse (sequences x q_heads, fp32) receives the logarithm of the softmax's sum."""
         self._here(cache)
-        heads, rest = divmod(Q.shape[1], cache.head_dim)
-        if rest:
-            raise ValueError("the width of Q must be a multiple of head_dim")
-        dt, code = Q.dtype, _code_of(Q)
-        q, ldq = self._rows(Q, "Q", dt, cache.seqs, Q.shape[1])
-        o, ldo = self._rows(O, "O", dt, cache.seqs, Q.shape[1])
-        ln = self._vector(lengths, "lengths", torch.int32, cache.seqs)
-        ls = self._vector(lse, "lse", torch.float32, cache.seqs * heads) if lse is not None else None
-        self._check(self._lib.gelo_paged_attention(self._h, cache.ref, q, ldq, heads, ln, cache.default_scale if scale is None else scale,
-                                                   window, code, o, ldo, ls, self._on(stream)), "gelo_paged_attention")
+        self._check(_marshal.paged_attention(self._handle, self.device, cache.ref, Q, lengths, O, cache.default_scale if scale is None else scale,
+                                             window, lse, stream), "gelo_paged_attention")
 
     def unmix(self, Ainv, lda, Yp, n, k, p, dtype, Q, K=None, V=None, stream=None):
         self._check(self._lib.gelo_unmix(self._h, _ptr(Ainv), lda, _ptr(Yp), n, k, p, dtype_code(dtype),

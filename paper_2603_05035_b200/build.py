@@ -1,4 +1,5 @@
-"""Builds ``libgelo.so`` (sm_100a only) from ``csrc/*.cu`` with nvcc, in-tree.
+"""Builds ``libgelo.so`` (sm_100a only) from ``csrc/*.cu`` with nvcc, in-tree, and ``_marshal.so``, which hands torch tensors to it, from
+``csrc/marshal.cpp`` with the host compiler.
 
     python -m paper_2603_05035_b200.build [--force]
 """
@@ -14,6 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgelo.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -58,7 +60,31 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".{os.getpid()}.tmp"
         subprocess.check_call([_nvcc(), "-shared", "-o", tmp, *objs, "-lcudart"])
         os.replace(tmp, LIB)
+    _build_marshal(force)
     return LIB
+
+
+def _build_marshal(force: bool) -> None:
+    """``_marshal.so``: a Python module on torch's C++ tensors, linked against the ``libgelo.so`` beside it."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    if not (force or _stale(MARSHAL, [src, os.path.join(HERE, "..", "include", "gelo.h")])):
+        return
+    import sysconfig
+
+    import torch
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    torch_dir = os.path.dirname(torch.__file__)
+    torch_lib, torch_include = os.path.join(torch_dir, "lib"), os.path.join(torch_dir, "include")
+    tmp = MARSHAL + f".{os.getpid()}.tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", torch_include, "-isystem", os.path.join(torch_include, "torch", "csrc", "api", "include"), "-isystem", os.path.join(cuda, "include"),
+           "-isystem", sysconfig.get_paths()["include"], src, "-o", tmp, f"-L{HERE}", "-l:libgelo.so", f"-L{torch_lib}", "-lc10", "-lc10_cuda",
+           "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{torch_lib}"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("g++ failed: " + " ".join(cmd))
+    os.replace(tmp, MARSHAL)
 
 
 if __name__ == "__main__":

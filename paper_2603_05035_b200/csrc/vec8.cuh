@@ -17,6 +17,22 @@ __device__ __forceinline__ void round_to(float v, float* out) { *out = v; }
 __device__ __forceinline__ void round_to(float v, __nv_bfloat16* out) { *out = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void round_to(float v, __half* out) { *out = __float2half_rn(v); }
 
+// two values rounded to a 16-bit type, the first in the low half
+template <typename T>
+__device__ __forceinline__ uint32_t two_of(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t two_of<__nv_bfloat16>(float a, float b)
+{
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+template <>
+__device__ __forceinline__ uint32_t two_of<__half>(float a, float b)
+{
+    const __half2 t = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+
 template <typename T>
 struct Eight {
     uint4 raw[sizeof(T) / 2];
@@ -37,8 +53,13 @@ struct Eight {
     }
     __device__ __forceinline__ void narrow(const float (&v)[8])
     {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) round_to(v[j], reinterpret_cast<T*>(raw) + j);
+            for (int j = 0; j < 8; ++j) reinterpret_cast<float*>(raw)[j] = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) reinterpret_cast<uint32_t*>(raw)[j] = two_of<T>(v[2 * j], v[2 * j + 1]);
+        }
     }
 };
 
