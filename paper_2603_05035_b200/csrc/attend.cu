@@ -23,10 +23,10 @@ namespace gelo {
 namespace {
 
 constexpr int kMaxCtas = 320;
-constexpr int kLeast = 4;                                     // tiles that a warp takes where heads are cut
+constexpr int kLeast = 2;                                     // tiles that a warp takes where heads are cut
 constexpr int kWhole = 24;                                    // up to so many tiles a head stays in one piece
 constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
-constexpr int kMaxParts = 64;                                 // a head's sums come from no more than about so many CTAs
+constexpr int kMaxParts = 40;                                 // a head's sums come from no more than about so many CTAs
 constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
 constexpr float kNone = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -162,6 +162,10 @@ __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there, uint64_t once)
 {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(once) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint64_t once)
+{
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(once) : "memory");
 }
 __device__ __forceinline__ uint64_t read_once()
 {
@@ -796,7 +800,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const long long at = on ? t.page * p.page_stride + t.in_page * p.token_stride : 0;
         const uint32_t dst = ring + stage * G::kStage;
         if (G::kPieces <= 32 && p.page_size % 16 == 0) {      // sixteen positions are neighbours on one page
-            const bool wanted = 16 * my_piece < p.dh * kBytes;
+            const bool wanted = 16 * my_piece < p.dh * kBytes, full_rows = p.dh == G::kWidth;
 #pragma unroll
             for (int b = 0; b < kTile / 16; ++b) {
                 // the page is that of any position that counts; positions before it on the page may not count, but lie there
@@ -804,6 +808,19 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 const int one = half ? __ffs(half) - 1 : 0;
                 const long long from = __shfl_sync(0xffffffffu, at, 16 * b + one) - (half ? one * p.token_stride : 0) + my_at;
                 const char *k = t.keys + from, *v = t.values + from;
+                const uint32_t base = dst + G::piece(16 * b + my_row, my_piece);
+                if (half == 0xffffu && full_rows) {           // nearly always: nothing to leave out
+#pragma unroll
+                    for (int i = 0; i < 16 / kRowsACopy; ++i) {
+                        // (rows that a copy apart lie eight apart have their pieces in one order, others in an order of their own)
+                        const uint32_t to = kRowsACopy % 8 == 0 ? base + i * kRowsACopy * G::kRow : dst + G::piece(16 * b + i * kRowsACopy + my_row, my_piece);
+                        copy16(to, k, once);
+                        copy16(to + G::kHalf, v, once);
+                        k += kRowsACopy * p.token_stride;
+                        v += kRowsACopy * p.token_stride;
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int i = 0; i < 16 / kRowsACopy; ++i) {
                     const int row = i * kRowsACopy + my_row;
@@ -943,7 +960,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             float top = kNone, total = 0.0f;
             float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (works) {
-                constexpr int kBatch = 8;
+                constexpr int kBatch = 16;
                 for (int a = u.first + group; a <= u.last; a += kBatch * groups) {
                     float2 t[kBatch];
                     float4 v[kBatch];
