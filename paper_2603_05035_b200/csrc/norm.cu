@@ -82,30 +82,35 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= u[j];
     };
-    auto collect = [&](int g, const float (&v)[8]) {
+    auto store = [&](void* to, int ld, int g, const float (&v)[8], float factor) {
+        float u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = v[j] * factor;
+        Eight<T> a;
+        a.narrow(u);
+        a.store(static_cast<T*>(to) + (size_t)row * ld + 8 * g);
+    };
+    auto collect = [&](int g, float (&v)[8]) {                // leaves h w in v
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
+        weigh(g, v);
         if (p.codes) {
-            float u[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = v[j];
-            weigh(g, u);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(u[j]));
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
         }
     };
 
     if constexpr (kVecs > 0) {
 #pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (t + i * kThreads < groups) load(t + i * kThreads, h[i]);
+#pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             const int g = t + i * kThreads;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) h[i][j] = 0.0f;
-            if (g < groups) load(g, h[i]);
+            if (g >= groups) continue;
+            if (p.r_out) store(p.r_out, p.ldro, g, h[i], 1.0f);       // (x and r of this place have been read, whichever of them it is)
+            collect(g, h[i]);
         }
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-            if (t + i * kThreads < groups) collect(t + i * kThreads, h[i]);
     } else {
         for (int g = t; g < groups; g += kThreads) {
             load(g, h[0]);
@@ -123,20 +128,8 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
         if (t == 0) p.row_scale[row] = scale;
     }
 
-    auto emit = [&](int g, float (&v)[8]) {
-        Eight<T> a;
-        if (p.r_out) {
-            a.narrow(v);
-            a.store(static_cast<T*>(p.r_out) + (size_t)row * p.ldro + 8 * g);
-        }
-        weigh(g, v);
-        if (p.y) {
-            float u[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = v[j] * inv;
-            a.narrow(u);
-            a.store(static_cast<T*>(p.y) + (size_t)row * p.ldy + 8 * g);
-        }
+    auto emit = [&](int g, float (&v)[8]) {                   // v: h w
+        if (p.y) store(p.y, p.ldy, g, v, inv);
         if (p.codes) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= to_code;
@@ -150,6 +143,8 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
     } else {
         for (int g = t; g < groups; g += kThreads) {
             load(g, h[0]);
+            if (p.r_out) store(p.r_out, p.ldro, g, h[0], 1.0f);
+            weigh(g, h[0]);
             emit(g, h[0]);
         }
     }
@@ -166,10 +161,16 @@ int launch_as(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
 template <typename T>
 int launch_typed(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
 {
+    // A warp a row up to 512 values; then as many threads as leave each one or two groups, since a row waits for its slowest thread and more
+    // threads in flight read more (4096 rows of 4096 bf16: 256 threads of two groups 24.2 us, 128 of four 26.5, 64 of eight 33, 512 of one 24.8;
+    // of 8192: 512 of two 46, 256 of four 49; of 2048: 256 of one 12.8, 128 of two 13.1).
     const int groups = p.d / 8;
     if (groups <= 32) return launch_as<T, 32, 1>(ctx, p, st);
-    if (groups <= 128) return launch_as<T, 32, 4>(ctx, p, st);
+    if (groups <= 64) return launch_as<T, 32, 2>(ctx, p, st);
+    if (groups <= 128) return launch_as<T, 128, 1>(ctx, p, st);
+    if (groups <= 256) return launch_as<T, 256, 1>(ctx, p, st);
     if (groups <= 512) return launch_as<T, 256, 2>(ctx, p, st);
+    if (groups <= 1024) return launch_as<T, 512, 2>(ctx, p, st);
     if (groups <= 2048) return launch_as<T, 512, 4>(ctx, p, st);
     return launch_as<T, 512, 0>(ctx, p, st);
 }
