@@ -429,8 +429,9 @@ int gelo_append_kv(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* K_dev,
  * (window 0: all):   o = sum_j p_j v_j,  p = softmax_j(scale q . k_j).   O_dev: rows as Q_dev (may be Q_dev itself with the same stride).
  * lse_dev (optional, seqs x q_heads floats): log sum_j exp(scale q . k_j).  A length of zero or less gives o = 0 and lse = -infinity.
  * Entries of the cache outside those positions are not read, or do not count whatever they hold.  A length beyond the table is cut to it, and a page
- * outside the cache counts as absent; both record GELO_ERR_INVALID.  Rows of one call may share pages.  Needs a workspace
- * of gelo_attention_workspace_bytes() bytes, whatever the sizes.  Results do not depend on what runs beside the call. */
+ * outside the cache counts as absent; both record GELO_ERR_INVALID.  A key whose logit is minus infinity does not count either; an infinity
+ * among the values that count makes its component infinite or NaN.  Sequences may share pages.  The same inputs give the same bytes.  Needs a
+ * workspace of gelo_attention_workspace_bytes() bytes, whatever the sizes. */
 size_t gelo_attention_workspace_bytes(void);
 int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* Q_dev, int ldq, int q_heads, const int* len_dev,
                          float scale, int window, int dtype, void* O_dev, int ldo, float* lse_dev, void* stream);

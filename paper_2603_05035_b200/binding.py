@@ -377,8 +377,8 @@ class Context:
 
     def project_e4m3_rows(self, U8, u_scale, W8, w_scale, m, d, p, Yp, stream=None):
         """Yp (bf16) = u_scale[:, None] * w_scale * (U8 @ W8) on E4M3 operands: a scale per row of U8 (as rms_norm leaves them)."""
-        self._check(self._lib.gelo_project_e4m3_rows(self._h, _ptr(U8), _ptr(u_scale), _ptr(W8), _ptr(w_scale), m, d, p, _ptr(Yp),
-                                                     _stream(stream)), "gelo_project_e4m3_rows")
+        self._check(_marshal.project_e4m3_rows(self._handle, self.device, U8, u_scale, W8, w_scale, m, d, p, Yp, stream),
+                    "gelo_project_e4m3_rows")
 
     # ---- around the projection -------------------------------------------------------------
     def _here(self, cache):

@@ -163,6 +163,28 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// E4M3 codes: bytes, or torch's type for them
+const void* codes_of(PyObject* o, const char* name, int64_t count, int device)
+{
+    const at::ScalarType t = tensor(o, name).scalar_type();
+    return values_of<void>(o, name, t == at::kFloat8_e4m3fn ? t : at::kByte, count, device);
+}
+
+// (context, device, U8, u_scale, W8, w_scale, m, d, p, Yp, stream)
+PyObject* project_e4m3_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 11, [&] {
+        const int device = whole(a[1]), m = whole(a[6]), d = whole(a[7]), p = whole(a[8]);
+        const void* u = codes_of(a[2], "U8", (int64_t)m * d, device);
+        const float* su = values_of<float>(a[3], "u_scale", at::kFloat, m, device);
+        const void* w = codes_of(a[4], "W8", (int64_t)d * p, device);
+        const at::Tensor& sw = tensor(a[5], "w_scale");                                // one value, or the pair that the quantiser leaves
+        const float* scale = values_of<float>(a[5], "w_scale", at::kFloat, sw.numel() == 2 ? 2 : 1, device);
+        void* y = values_of<void>(a[9], "Yp", at::kBFloat16, (int64_t)m * p, device);
+        return gelo_project_e4m3_rows(context(a[0]), u, su, w, scale, m, d, p, y, stream_of(a[10], device));
+    });
+}
+
 // (context, device, X, heads, pos, rope, Y, stream)
 PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -236,6 +258,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
 
 PyMethodDef methods[] = {
     {"rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm)), METH_FASTCALL, nullptr},
+    {"project_e4m3_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(project_e4m3_rows)), METH_FASTCALL, nullptr},
     {"rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotary)), METH_FASTCALL, nullptr},
     {"append_kv", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(append_kv)), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},

@@ -123,3 +123,33 @@ def test_descriptions_of_tensors_that_do_not_fit():
         binding.PagedCache(k.double(), k, table)
     with pytest.raises(ValueError):
         binding.Rope(torch.zeros(32, dtype=torch.float64))
+
+
+def test_marshalling_looks_before_it_calls(lib, ctx):
+    """Tensors of the wrong kind are refused in words before the library sees an address."""
+    m = binding._marshal
+    handle = ctypes.addressof(ctx)
+    x = torch.zeros((4, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="X must be 4 x 64 of BFloat16 on cuda:0"):
+        m.rms_norm(handle, 0, x, x, None, 1e-5, None, None, None, None, 0)
+    with pytest.raises(ValueError, match="unsupported dtype of X"):
+        m.rms_norm(handle, 0, x.double(), x, None, 1e-5, None, None, None, None, 0)
+    with pytest.raises(ValueError, match="X"):
+        m.rms_norm(handle, 0, x[0], x, None, 1e-5, None, None, None, None, 0)
+    with pytest.raises(ValueError, match="X must be"):
+        m.rms_norm(handle, 0, "x", x, None, 1e-5, None, None, None, None, 0)
+    with pytest.raises(TypeError):
+        m.rms_norm(handle, 0, x)
+    with pytest.raises(ValueError, match="multiple of heads"):
+        m.rotary(handle, 0, x, 3, x, 0, None, 0)
+    c = cache()
+    with pytest.raises(ValueError, match="multiple of head_dim"):
+        m.paged_attention(handle, 0, ctypes.addressof(c), x, x, x, 0.1, 0, None, 0)
+    with pytest.raises(ValueError, match="K must be"):
+        m.append_kv(handle, 0, ctypes.addressof(c), x, x, x, None, None, None, None, 0)
+    with pytest.raises(ValueError, match="U8 must hold"):
+        m.project_e4m3_rows(handle, 0, x, x, x, x, 4, 64, 64, x, 0)
+    with pytest.raises((TypeError, ValueError)):
+        m.paged_attention(handle, 0, "cache", x, x, x, 0.1, 0, None, 0)
+    with pytest.raises(ValueError, match="out of range"):
+        m.rotary(handle, 0, x, 1 << 40, x, 0, None, 0)

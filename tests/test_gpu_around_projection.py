@@ -372,6 +372,19 @@ def test_attention_shares_of_many_sequences(ctx, dt, cache):
 
 
 @pytest.mark.parametrize("dt,cache", TYPES)
+@pytest.mark.parametrize("seqs,hq,hk,dh,ps,longest", [(650, 1, 1, 64, 16, 190), (300, 6, 2, 128, 16, 380), (200, 48, 3, 80, 8, 60), (130, 5, 5, 256, 32, 100),
+                                                      (2500, 1, 1, 16, 4, 9)])
+def test_attention_of_many_short_sequences(ctx, dt, cache, seqs, hq, hk, dh, ps, longest):
+    """So many short heads that every warp takes some of its own, lengths of zero among them; fewer, and a CTA takes each."""
+    lens = [(37 * i * i + 11 * i) % (longest + 1) for i in range(seqs)]
+    paged, _ = filled(seqs, lens, ps, hk, dh, "token", cache)
+    Q = rnd(47, seqs, hq * dh, scale=2.0, dtype=dt)
+    check_attention(ctx, paged, Q, lens, dt, cache)
+    few = binding.PagedCache(paged.k, paged.v, paged.table[:70], paged.struct.k_scale, paged.struct.v_scale)
+    check_attention(ctx, few, Q[:70], lens[:70], dt, cache, window=33)
+
+
+@pytest.mark.parametrize("dt,cache", TYPES)
 def test_attention_pages_and_lengths_that_do_not_exist(ctx, dt, cache):
     lens = [100, 50, 64, 33]
     paged, _ = filled(11, lens, 16, 2, 64, "head", cache)
@@ -596,6 +609,15 @@ def test_refusals(ctx):
         ctx.paged_attention(paged, Q[:, :192], ln, torch.empty_like(Q)[:, :192])
     with pytest.raises(ValueError):
         ctx.paged_attention(paged, Q, ln.long(), torch.empty_like(Q))
+    u8, w8, y = torch.zeros((4, 64), dtype=torch.uint8, device="cuda"), torch.zeros((64, 32), dtype=torch.uint8, device="cuda"), torch.zeros((4, 32), dtype=torch.bfloat16, device="cuda")
+    su, sw = torch.ones(4, device="cuda"), torch.ones(2, device="cuda")
+    ctx.project_e4m3_rows(u8, su, w8, sw, 4, 64, 32, y)
+    ctx.project_e4m3_rows(u8.view(torch.float8_e4m3fn), su, w8, sw[:1], 4, 64, 32, y)
+    for bad in ((u8[:3], su, w8, sw, y), (u8, su[:3], w8, sw, y), (u8, su, w8.float(), sw, y), (u8, su, w8, torch.ones(3, device="cuda"), y), (u8, su, w8, sw, y.float())):
+        with pytest.raises(ValueError):
+            ctx.project_e4m3_rows(*bad[:4], 4, 64, 32, bad[4])
+    with pytest.raises(ValueError):
+        ctx.paged_attention(paged, Q, ln, torch.empty_like(Q), window=1 << 40)
     with pytest.raises(ValueError):
         binding.PagedCache(paged.k, paged.v, paged.table.expand(2, -1)[:1].expand(2, -1))
     with pytest.raises(binding.GeloError):                     # more tokens than sequences and no list of them
