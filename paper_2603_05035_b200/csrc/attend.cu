@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kMaxCtas = 320;
 constexpr int kLeast = 2;                                     // tiles that a warp takes where heads are cut
-constexpr int kWhole = 24;                                    // up to so many tiles a head stays in one piece
+constexpr int kWhole = 24, kWholeFew = 56;                     // up to so many tiles a head stays in one piece; with no more heads than CTAs
 constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
 constexpr int kMaxParts = 40;                                 // a head's sums come from no more than about so many CTAs
 constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
@@ -720,7 +720,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         all += prefix.warps[w];
         longest = max(longest, prefix.longest[w]);
     }
-    const bool whole = longest <= kWhole, alone = whole && (long long)p.seqs * p.units >= 2 * (long long)gridDim.x;
+    const long long heads_in_all = (long long)p.seqs * p.units;
+    const bool whole = longest <= (heads_in_all <= gridDim.x ? kWholeFew : kWhole), alone = whole && heads_in_all >= 2 * (long long)gridDim.x;
     const int cost = alone ? kAloneCost : kSegmentCost, team = alone ? 1 : kWarps, member = alone ? 0 : warp;
     const long long total = (all + (long long)cost * p.seqs) * p.units;
     long long share = quotient(total + gridDim.x * (alone ? kWarps : 1) - 1, gridDim.x * (alone ? kWarps : 1));
