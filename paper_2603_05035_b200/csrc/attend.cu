@@ -26,6 +26,7 @@ constexpr int kMaxCtas = 320;
 constexpr int kLeast = 2;                                     // tiles that a warp takes where heads are cut
 constexpr int kWhole = 24, kWholeFew = 56;                     // up to so many tiles a head stays in one piece; with no more heads than CTAs
 constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
+constexpr int kPieceSlack = 16;                               // equal pieces may be larger than a share by this part of it
 constexpr int kMaxParts = 40;                                 // a head's sums come from no more than about so many CTAs
 constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
 constexpr float kNone = -INFINITY;
@@ -730,18 +731,52 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const long long average = quotient(all + p.seqs - 1, p.seqs);
         share = max(share, max(min((long long)kLeast * kWarps, average), (average + kMaxParts - 1) / kMaxParts) + cost);
     }
-    const long long x0 = (alone ? warp * (long long)gridDim.x + cta : cta) * share;
-    if (x0 >= total) return;                                  // (where not alone, all of the CTA; warps that are alone meet at no barrier)
+    // Few sequences: their heads in equal pieces, one for a CTA, if pieces not much larger than a share find a CTA each.  No CTA then has
+    // the end of one head and the beginning of another to see to.
+    int piece_first = -1, piece_last = -1;                    // the CTAs that a head's pieces belong to
     Walk<kTile> ahead, walk;
-    {
+    if (!whole && p.seqs <= 32 && heads_in_all <= (long long)gridDim.x) {
+        int n = 0;
+        if (lane < p.seqs) {
+            const Span sp = span_of<kTile>(p, lane);
+            n = sp.t1 - sp.t0;
+        }
+        const int grid = (int)gridDim.x, units = p.units, even = (int)min(quotient(all * units + grid - 1, grid), (long long)INT_MAX / 4);
+        const int least = max(max(kLeast * kWarps, (longest + kMaxParts - 1) / kMaxParts), even), size = least + (int)((long long)least * lane / 32);
+        int count = 0;                                        // pieces of this lane's size (the heads are as many as CTAs at most, so no sum gets far)
+        for (int s = 0; s < p.seqs; ++s) count += min((__shfl_sync(0xffffffffu, n, s) + size - 1) / size, grid + 1);
+        const uint32_t fit = __ballot_sync(0xffffffffu, (long long)count * units <= grid && size <= share + max(4ll, share / kPieceSlack));
+        if (fit) {
+            const int best = __shfl_sync(0xffffffffu, size, __ffs(fit) - 1), mine = (n + best - 1) / best;
+            int upto = mine * units;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, upto, off);
+                if (lane >= off) upto += u;
+            }
+            const int seq = __popc(__ballot_sync(0xffffffffu, upto <= cta));
+            if (seq >= p.seqs) return;                        // (all of the CTA)
+            const int pieces = __shfl_sync(0xffffffffu, mine, seq), tiles = __shfl_sync(0xffffffffu, n, seq);
+            const int at = cta - (__shfl_sync(0xffffffffu, upto, seq) - pieces * units), unit = at / pieces, piece = at - unit * pieces;
+            piece_first = cta - piece;
+            piece_last = piece_first + pieces - 1;
+            const Place from = {seq, unit, (int)((long long)tiles * piece / pieces)};
+            Place to = {seq, unit, (int)((long long)tiles * (piece + 1) / pieces)};
+            if (to.tile == tiles) to = unit + 1 < units ? Place{seq, unit + 1, 0} : Place{seq + 1, 0, 0};
+            ahead.begin(p, from, 0, to);
+        }
+    }
+    if (piece_first < 0) {
+        const long long x0 = (alone ? warp * (long long)gridDim.x + cta : cta) * share;
+        if (x0 >= total) return;                              // (where not alone, all of the CTA; warps that are alone meet at no barrier)
         long long from_at, to_at;
         const Place from = prefix.template find<kTile>(p, x0, per, cost, whole, lane, from_at);
         Place to = {p.seqs, 0, 0};
         if (x0 + share < total) to = prefix.template find<kTile>(p, x0 + share, per, cost, whole, lane, to_at);
         if (from.seq == to.seq && from.unit == to.unit && from.tile == to.tile) return;
         ahead.begin(p, from, from_at, to);
-        walk = ahead;
     }
+    walk = ahead;
 
     // ---- copies: the tiles that this warp will take, in order, kStages - 1 of them ahead ----
     const uint32_t ring = smem_at(smem) + warp * kStages * G::kStage;
@@ -899,7 +934,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const int n = done.s.t1 - done.s.t0;
         const bool in_one = done.end - done.at == n;
         const long long unit_at = done.seq_at + (long long)done.unit * (n + cost) + cost;
-        const int first_cta = in_one ? cta : (int)quotient(unit_at, share), last_cta = in_one ? cta : (int)quotient(unit_at + n - 1, share);
+        const int first_cta = in_one ? cta : piece_first >= 0 ? piece_first : (int)quotient(unit_at, share);
+        const int last_cta = in_one ? cta : piece_first >= 0 ? piece_last : (int)quotient(unit_at + n - 1, share);
         float* slot = p.slots + (size_t)(2 * cta + (first_cta == cta ? 1 : 0)) * p.slot;
         if (tid < done_heads) {
             const float total = all.total(tid);
