@@ -3,7 +3,10 @@
 // A CTA takes one token: its threads first work out the cosines and sines of all pairs, which all heads share, then stream the heads
 // of Q, K and V through.  position * turns is formed and reduced to one circle in binary64 (a position times an fp32 frequency is off
 // by position * 2^-24), and so are the cosine and sine, which are then rounded once; the rest is fp32.  Every pair belongs to one thread, which reads both values before it writes either, so Q may be
-// rotated in place.  Bound by HBM: Q, K and V in, all three out.
+// rotated in place.  Bound by HBM: Q, K and V in, all three out.  4096 tokens of 32 heads of 128 in bf16, 201 MB: 37.5 us, 82% of a copy's rate; 64 tokens 4 us.
+// Threads take the pieces of all heads in a simple loop: a thread that holds several pieces in flight takes the registers of
+// the warps that hide the loads (two to four pieces 43 to 66 us), and fewer instructions per piece gain nothing.
+// Pieces are eight components wide where the layout allows it (interleaved, or a `rot` of whole sixteens: 112 of 128 43 us), else one (120 of 128 82 us).
 #include "common.cuh"
 #include "vec8.cuh"
 
