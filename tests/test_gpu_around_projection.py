@@ -322,6 +322,15 @@ def check_attention(ctx, paged, Q, lens, dt, cache, scale=None, window=0, status
     return o, lse[:seqs]
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dh", [8, 24, 72])
+def test_attention_of_narrow_heads(ctx, dt, dh):
+    """Widths that are no multiple of 16."""
+    lens = [70, 0, 1, 33]
+    paged, _ = filled(dh, lens, 3, 2, dh, "wide", dt)
+    check_attention(ctx, paged, rnd(48, 4, 6 * dh, scale=2.0, dtype=dt), lens, dt, dt)
+
+
 TYPES = [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")]
 
 
