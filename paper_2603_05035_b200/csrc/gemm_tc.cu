@@ -1479,8 +1479,11 @@ int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda
     if ((lda % 16) || (ldb % 16) || (ldc % 8) || (N % 8) || !aligned16(A8) || !aligned16(B8) || !aligned16(C) || !sa || !sb)
         return GELO_ERR_INVALID;
     EncodeTiledFn enc = reinterpret_cast<EncodeTiledFn>(ctx->tmap_encode);
-    // narrow tiles while they still find an SM each: W is then streamed by twice as many SMs (64 rows, K = 4096, N = 12288)
-    const bool narrow = ceil_div(M, BM) * ceil_div(N, 128) <= ctx->sm_count;
+    // Narrow tiles while they still find an SM each: W is then streamed by twice as many SMs (K = 4096, N = 12288: 64 rows 18.3 -> 15.0 us; 1075 rows,
+    // N = 1424 17.3 -> 15.3), unless so many SMs ask for the same few lines of A that they wait for one another (8 rows, N = 12288: 18.1
+    // with wide tiles, 20.9 with narrow ones; N = 8192: 17.2, 15.6).
+    const int narrow_tiles = ceil_div(M, BM) * ceil_div(N, 128);
+    const bool narrow = narrow_tiles <= ctx->sm_count && (M >= 32 || narrow_tiles <= 72);
     const bool pair = !narrow && use_pair(ctx, M, N, 1, false, TC_STORE_BF16);
     CUtensorMap ma, mb;
     {
