@@ -124,14 +124,30 @@ struct Walk {
     }
 };
 
+// The place at weight x of the line, in which a head of n - cost tiles weighs n; where nothing is cut, the first head that begins at x or behind.  x lies in
+// sequence seq, which begins at seq_at (that of the place in the end).
+__device__ __forceinline__ Place place_in(const AttendArgs& p, long long x, int seq, int n, int cost, bool whole, long long& seq_at)
+{
+    Place at;
+    at.seq = seq;
+    at.unit = (int)quotient(x - seq_at, n);
+    const int offset = (int)(x - seq_at - (long long)at.unit * n);
+    at.tile = whole ? 0 : max(offset - cost, 0);
+    if (whole && offset > 0 && ++at.unit == p.units) {
+        at.unit = 0;
+        ++at.seq;
+        seq_at += (long long)n * p.units;
+    }
+    return at;
+}
+
 // The lengths of all sequences as a CTA's threads have added them up: thread i those of the sequences from i * per on
 template <int kWarps>
 struct Prefix {
     long long inside[32 * kWarps];                            // tiles of a head before a thread's first sequence, of its warp's alone
     long long warps[kWarps];                                  // tiles of a head of a warp's sequences
     int longest[kWarps];
-    // The place at weight x of the line, in which a head of n tiles weighs n + cost; where nothing is cut, the first head that begins at x or behind.
-    // A warp works it out together; seq_at: the weight before the place's sequence.
+    // The place at weight x of the line (place_in), which a warp works out together; seq_at: the weight before the place's sequence
     template <int kTile>
     __device__ __forceinline__ Place find(const AttendArgs& p, long long x, int per, int cost, bool whole, int lane, long long& seq_at) const
     {
@@ -159,15 +175,7 @@ struct Prefix {
             seq_at += (long long)n * p.units;
             ++at.seq;
         }
-        at.unit = (int)quotient(x - seq_at, n);
-        const int offset = (int)(x - seq_at - (long long)at.unit * n);
-        at.tile = whole ? 0 : max(offset - cost, 0);
-        if (whole && offset > 0 && ++at.unit == p.units) {
-            at.unit = 0;
-            ++at.seq;
-            seq_at += (long long)n * p.units;
-        }
-        return at;
+        return place_in(p, x, at.seq, n, cost, whole, seq_at);
     }
 };
 
@@ -705,10 +713,27 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
 
     // ---- this CTA's share of the line of tiles, or where `alone` this warp's ----
+    // Up to 32 sequences: each lane of every warp has one, and no warp waits for another; more: the threads of the CTA add them up together.
+    const bool few = p.seqs <= 32;
     const int per = (p.seqs + kThreads - 1) / kThreads;
-    {
+    long long all = 0, before = 0;                            // tiles of a head of all sequences; of those before this lane's
+    int longest = 0, n = 0;                                   // of this lane's
+    if (few) {
+        if (lane < p.seqs) {
+            const Span sp = span_of<kTile>(p, lane);
+            n = sp.t1 - sp.t0;
+        }
+        long long upto = n;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += u;
+        }
+        before = upto - n;
+        all = __shfl_sync(0xffffffffu, upto, 31);
+        longest = __reduce_max_sync(0xffffffffu, n);
+    } else {
         long long mine = 0;
-        int longest = 0;
         for (int s = min(tid * per, p.seqs); s < min((tid + 1) * per, p.seqs); ++s) {
             const Span sp = span_of<kTile>(p, s);
             mine += sp.t1 - sp.t0;
@@ -727,13 +752,11 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
             prefix.longest[warp] = longest;
         }
         __syncthreads();
-    }
-    long long all = 0;
-    int longest = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        all += prefix.warps[w];
-        longest = max(longest, prefix.longest[w]);
+        for (int w = 0; w < kWarps; ++w) {
+            all += prefix.warps[w];
+            longest = max(longest, prefix.longest[w]);
+        }
     }
     const long long heads_in_all = (long long)p.seqs * p.units;
     const bool whole = longest <= (heads_in_all <= gridDim.x ? kWholeFew : kWhole), alone = whole && heads_in_all >= 2 * (long long)gridDim.x;
@@ -749,12 +772,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     // the end of one head and the beginning of another to see to.
     int piece_first = -1, piece_last = -1;                    // the CTAs that a head's pieces belong to
     Walk<kTile> ahead, walk;
-    if (!whole && p.seqs <= 32 && heads_in_all <= (long long)gridDim.x) {
-        int n = 0;
-        if (lane < p.seqs) {
-            const Span sp = span_of<kTile>(p, lane);
-            n = sp.t1 - sp.t0;
-        }
+    if (!whole && few && heads_in_all <= (long long)gridDim.x) {
         const int grid = (int)gridDim.x, units = p.units, even = (int)min(quotient(all * units + grid - 1, grid), (long long)INT_MAX / 4);
         const int least = max(max(kLeast * kWarps, (longest + kMaxParts - 1) / kMaxParts), even), size = least + (int)((long long)least * lane / 32);
         int count = 0;                                        // pieces of this lane's size (the heads are as many as CTAs at most, so no sum gets far)
@@ -784,9 +802,16 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const long long x0 = (alone ? warp * (long long)gridDim.x + cta : cta) * share;
         if (x0 >= total) return;                              // (where not alone, all of the CTA; warps that are alone meet at no barrier)
         long long from_at, to_at;
-        const Place from = prefix.template find<kTile>(p, x0, per, cost, whole, lane, from_at);
+        const long long mine_at = (before + (long long)cost * lane) * p.units;         // (few)
+        auto find = [&](long long x, long long& seq_at) {
+            if (!few) return prefix.template find<kTile>(p, x, per, cost, whole, lane, seq_at);
+            const int seq = __popc(__ballot_sync(0xffffffffu, lane < p.seqs && mine_at <= x)) - 1;
+            seq_at = __shfl_sync(0xffffffffu, mine_at, seq);
+            return place_in(p, x, seq, __shfl_sync(0xffffffffu, n, seq) + cost, cost, whole, seq_at);
+        };
+        const Place from = find(x0, from_at);
         Place to = {p.seqs, 0, 0};
-        if (x0 + share < total) to = prefix.template find<kTile>(p, x0 + share, per, cost, whole, lane, to_at);
+        if (x0 + share < total) to = find(x0 + share, to_at);
         if (from.seq == to.seq && from.unit == to.unit && from.tile == to.tile) return;
         ahead.begin(p, from, from_at, to);
     }
@@ -985,20 +1010,22 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
 
     // ---- heads that several CTAs share, the first and the last of this one's at most: who arrives last adds up, in the order of the CTAs ----
     if (cuts[0].heads + cuts[1].heads == 0) return;
-    __threadfence();
-    __syncthreads();
-    if (tid < 2) {
-        const Cut c = tid ? cuts[1] : cuts[0];
+    __syncthreads();                                          // what the CTA's threads have written is before the first warp's fence ...
+    if (warp == 0) {
+        __threadfence();
         bool mine = false;
-        if (c.heads > 0) {
-            mine = atomicAdd(p.arrived + c.first, 1) == c.last - c.first;
-            if (mine) p.arrived[c.first] = 0;
+        if (lane < 2) {
+            const Cut c = lane ? cuts[1] : cuts[0];
+            if (c.heads > 0) {
+                mine = atomicAdd(p.arrived + c.first, 1) == c.last - c.first;
+                if (mine) p.arrived[c.first] = 0;
+            }
+            last[lane] = mine;
         }
-        last[tid] = mine;
+        __threadfence();                                      // ... and what other CTAs wrote before they arrived is before what follows the barrier
     }
     __syncthreads();
     if (!last[0] && !last[1]) return;
-    __threadfence();
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
         if (!last[k]) continue;
