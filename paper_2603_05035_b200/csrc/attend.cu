@@ -58,12 +58,22 @@ struct AttendArgs {
     int slot;                                                 // floats
     int kv_heads, heads_a_unit, units;                        // units: heads_a_unit query heads of one key-value head each, per sequence
     float scale, v_scale;                                     // scale: of the logits, the keys' scale included
+    float a_seq, a_cta;                                       // 1 / seqs, 1 / CTAs
 };
 
 // a / b of non-negative numbers; nearly always both are small
 __device__ __forceinline__ long long quotient(long long a, long long b)
 {
     return ((a | b) >> 31) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
+// n / size rounded up, a_piece = 1 / size: the quotient in fp32 is off by one at most (n < 2^28, size >= 8), and put right
+__device__ __forceinline__ int pieces_of(int n, int size, float a_piece)
+{
+    int q = (int)((float)n * a_piece), rest = n - q * size;
+    if (rest < 0) { --q; rest += size; }
+    if (rest >= size) { ++q; rest -= size; }
+    return q + (rest > 0 ? 1 : 0);
 }
 
 // The positions that count of one sequence, and its tiles
@@ -765,21 +775,23 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     long long share = quotient(total + gridDim.x * (alone ? kWarps : 1) - 1, gridDim.x * (alone ? kWarps : 1));
     if (!whole) {
         // kLeast tiles for every warp, or an average head, since what a cut costs is more; and no head in many more than kMaxParts pieces
-        const long long average = quotient(all + p.seqs - 1, p.seqs);
-        share = max(share, max(min((long long)kLeast * kWarps, average), (average + kMaxParts - 1) / kMaxParts) + cost);
+        // (any share that is large enough will do: no division)
+        const float average = (float)all * p.a_seq;
+        share = max(share, (long long)fmaxf(fminf((float)(kLeast * kWarps), average), average * (1.0f / kMaxParts)) + 1 + cost);
     }
     // Few sequences: their heads in equal pieces, one for a CTA, if pieces not much larger than a share find a CTA each.  No CTA then has
     // the end of one head and the beginning of another to see to.
     int piece_first = -1, piece_last = -1;                    // the CTAs that a head's pieces belong to
     Walk<kTile> ahead, walk;
     if (!whole && few && heads_in_all <= (long long)gridDim.x) {
-        const int grid = (int)gridDim.x, units = p.units, even = (int)min(quotient(all * units + grid - 1, grid), (long long)INT_MAX / 4);
+        const int grid = (int)gridDim.x, units = p.units, even = (int)fminf((float)(all * units) * p.a_cta, (float)(INT_MAX / 4)) + 1;
         const int least = max(max(kLeast * kWarps, (longest + kMaxParts - 1) / kMaxParts), even), size = least + (int)((long long)least * lane / 32);
         int count = 0;                                        // pieces of this lane's size (the heads are as many as CTAs at most, so no sum gets far)
-        for (int s = 0; s < p.seqs; ++s) count += min((__shfl_sync(0xffffffffu, n, s) + size - 1) / size, grid + 1);
+        const float a_piece = 1.0f / (float)size;
+        for (int s = 0; s < p.seqs; ++s) count += min(pieces_of(__shfl_sync(0xffffffffu, n, s), size, a_piece), grid + 1);
         const uint32_t fit = __ballot_sync(0xffffffffu, (long long)count * units <= grid && size <= share + max(4ll, share / kPieceSlack));
         if (fit) {
-            const int best = __shfl_sync(0xffffffffu, size, __ffs(fit) - 1), mine = (n + best - 1) / best;
+            const int best = __shfl_sync(0xffffffffu, size, __ffs(fit) - 1), mine = pieces_of(n, best, 1.0f / (float)best);
             int upto = mine * units;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -1104,6 +1116,8 @@ int launch_as(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
         allowed.fetch_or(bit, std::memory_order_release);
     }
     const int ctas = G::kCtas * ctx->sm_count < kMaxCtas ? G::kCtas * ctx->sm_count : kMaxCtas;
+    p.a_seq = 1.0f / (float)p.seqs;
+    p.a_cta = 1.0f / (float)ctas;
     GELO_TRY(launch_chained(ctx, kernel, dim3(ctas), 32 * G::kWarps, G::kSmem, st, p));
     return after_launch(ctx);
 }
