@@ -56,7 +56,7 @@ struct AttendArgs {
     int ldq, ldo, q_heads, group, dh;
     int pages, page_size, page_shift, seqs, max_pages, table_ld, window;
     int slot;                                                 // floats
-    int kv_heads, heads_a_unit, units;                        // units: heads_a_unit query heads of one key-value head each, per sequence
+    int kv_heads, heads_a_unit, units, units_a_kv;            // units: heads_a_unit query heads of one key-value head each, per sequence
     float scale, v_scale;                                     // scale: of the logits, the keys' scale included
     float a_seq, a_cta;                                       // 1 / seqs, 1 / CTAs
 };
@@ -95,6 +95,8 @@ __device__ __forceinline__ Span span_of(const AttendArgs& p, int seq)
     s.t1 = max((s.len + kTile - 1) / kTile, s.t0 + 1);        // a sequence without positions has a tile too: its result has to be written
     return s;
 }
+
+__device__ __forceinline__ int kv_head_of(const AttendArgs& p, int unit) { return p.units_a_kv == 1 ? unit : unit / p.units_a_kv; }
 
 // A place in the line: tile `tile` (from its sequence's first) of (seq, unit)
 struct Place { int seq, unit, tile; };
@@ -239,22 +241,6 @@ __device__ __forceinline__ float power2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-template <typename M>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    M e[2];
-    round_to(lo, &e[0]);
-    round_to(hi, &e[1]);
-    return *reinterpret_cast<uint32_t*>(e);
-}
-// what rounding x to the 16-bit type leaves, rounded to it in turn
-template <typename M>
-__device__ __forceinline__ float rest(float x)
-{
-    M e;
-    round_to(x, &e);
-    return x - widen_at(&e, 0);
-}
 // four E4M3 codes as halves: the low two, the high two
 __device__ __forceinline__ void halves_of_codes(uint32_t four, uint32_t& low, uint32_t& high)
 {
@@ -377,7 +363,7 @@ struct MmaWarp {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const T* two = reinterpret_cast<const T*>(&qf[s][n][j]);
-                        qf[s][n][j] = pack2<M>(widen_at(two, 0) * down, widen_at(two, 1) * down);
+                        qf[s][n][j] = two_of<M>(widen_at(two, 0) * down, widen_at(two, 1) * down);
                     }
             }
             // columns 2t and 2t + 1 of a product are heads whose q other lanes hold
@@ -469,8 +455,12 @@ struct MmaWarp {
             }
 #pragma unroll
             for (int i = 0; i < 2 * kSub; ++i) {
-                ph[i >> 1][n][i & 1] = transposed(pack2<M>(e[i][0], e[i][1]));
-                if constexpr (kPair) pl[i >> 1][n][i & 1] = transposed(pack2<M>(rest<M>(e[i][0]), rest<M>(e[i][1])));
+                const uint32_t two = two_of<M>(e[i][0], e[i][1]);
+                ph[i >> 1][n][i & 1] = transposed(two);
+                if constexpr (kPair) {                        // what the rounding has left
+                    const M* const held = reinterpret_cast<const M*>(&two);
+                    pl[i >> 1][n][i & 1] = transposed(two_of<M>(e[i][0] - widen_at(held, 0), e[i][1] - widen_at(held, 1)));
+                }
             }
         }
         if (__any_sync(0xffffffffu, moved)) {
@@ -835,7 +825,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     W w;
     int first_head, heads;                                    // of the segment
     auto fetch = [&](const Walk<kTile>& at) {
-        const int per_kv = p.units / p.kv_heads, kv_head = at.unit / per_kv, head0 = (at.unit - kv_head * per_kv) * p.heads_a_unit;
+        const int kv_head = kv_head_of(p, at.unit), head0 = (at.unit - kv_head * p.units_a_kv) * p.heads_a_unit;
         heads = min(p.heads_a_unit, p.group - head0);
         first_head = kv_head * p.group + head0;
         w.fetch(p, static_cast<const T*>(p.q) + (size_t)at.seq * p.ldq + (size_t)first_head * p.dh, heads, lane);
@@ -843,15 +833,18 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     fetch(walk);
     int next_tile = ahead.at + member;
     bool more = true;
+    long long ahead_head = kv_head_of(p, ahead.unit) * p.head_stride;
     // The next two tiles whose copies have not been asked for: the page that each position (lane % kTile) is on is looked up that far ahead.
     struct Pending {
-        const char *keys, *values;                            // of the tile's head
+        long long head;                                       // where the tile's head lies in a page
         int page, in_page;
         bool any, on;                                         // there is a tile; this lane's position of it counts
-    } near = {nullptr, nullptr, 0, 0, false, false}, far = near;
+    } near = {0, 0, 0, false, false}, far = near;
     constexpr int kRowsACopy = 32 / G::kPieces ? 32 / G::kPieces : 1;                  // rows that one copy of the warp covers
     const int my_row = lane / G::kPieces, my_piece = lane % G::kPieces;
-    const long long my_at = my_row * p.token_stride + 16 * my_piece;
+    const long long my_at = my_row * p.token_stride + 16 * my_piece, step = kRowsACopy * p.token_stride;
+    const uint32_t my_place = G::piece(my_row, my_piece);
+    const bool wanted = 16 * my_piece < p.dh * kBytes, full_rows = p.dh == G::kWidth, neighbours = p.page_size % 16 == 0;
     const uint64_t once = read_once();
     auto copy_tile = [&](int stage) {                         // asks for the copies of the next tile and looks up the one after the one behind it
         const Pending t = near;
@@ -859,6 +852,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         while (more && next_tile >= ahead.end) {
             more = ahead.next(p, cost);
             next_tile = ahead.at + member;
+            ahead_head = kv_head_of(p, ahead.unit) * p.head_stride;
         }
         far.any = more;
         far.on = false;
@@ -870,9 +864,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 far.in_page = at - column * p.page_size;
                 far.page = p.table[(size_t)ahead.seq * p.table_ld + column];
             }
-            const long long head_at = (ahead.unit / (p.units / p.kv_heads)) * p.head_stride;
-            far.keys = static_cast<const char*>(p.k) + head_at;
-            far.values = static_cast<const char*>(p.v) + head_at;
+            far.head = ahead_head;
             next_tile += team;
         }
         if (!t.any) return;
@@ -884,39 +876,38 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         }
         const uint32_t who = __ballot_sync(0xffffffffu, on);
         if (lane == 0) counts[warp][stage] = who;
-        const long long at = on ? t.page * p.page_stride + t.in_page * p.token_stride : 0;
+        const long long at = (on ? t.page * p.page_stride + t.in_page * p.token_stride : 0) + t.head;
         const uint32_t dst = ring + stage * G::kStage;
-        if (G::kPieces <= 32 && p.page_size % 16 == 0) {      // sixteen positions are neighbours on one page
-            const bool wanted = 16 * my_piece < p.dh * kBytes, full_rows = p.dh == G::kWidth;
+        if (G::kPieces <= 32 && neighbours) {                 // sixteen positions are neighbours on one page
 #pragma unroll
             for (int b = 0; b < kTile / 16; ++b) {
-                // the page is that of any position that counts; positions before it on the page may not count, but lie there
-                const uint32_t half = (who >> (16 * b)) & 0xffffu;
-                const int one = half ? __ffs(half) - 1 : 0;
-                const long long from = __shfl_sync(0xffffffffu, at, 16 * b + one) - (half ? one * p.token_stride : 0) + my_at;
-                const char *k = t.keys + from, *v = t.values + from;
-                const uint32_t base = dst + G::piece(16 * b + my_row, my_piece);
+                const uint32_t half = (who >> (16 * b)) & 0xffffu, to = dst + 16 * b * G::kRow + my_place;
                 if (half == 0xffffu && full_rows) {           // nearly always: nothing to leave out
+                    const long long from = __shfl_sync(0xffffffffu, at, 16 * b) + my_at;
+                    const char *k = static_cast<const char*>(p.k) + from, *v = static_cast<const char*>(p.v) + from;
 #pragma unroll
                     for (int i = 0; i < 16 / kRowsACopy; ++i) {
-                        // (rows that a copy apart lie eight apart have their pieces in one order, others in an order of their own)
-                        const uint32_t to = kRowsACopy % 8 == 0 ? base + i * kRowsACopy * G::kRow : dst + G::piece(16 * b + i * kRowsACopy + my_row, my_piece);
-                        copy16(to, k, once);
-                        copy16(to + G::kHalf, v, once);
-                        k += kRowsACopy * p.token_stride;
-                        v += kRowsACopy * p.token_stride;
+                        // (a row's number and a lane's have no bit in common, so neither have their turns of the pieces)
+                        const uint32_t place = (to ^ G::piece(i * kRowsACopy, 0) % G::kRow) + i * kRowsACopy * G::kRow;
+                        copy16(place, k, once);
+                        copy16(place + G::kHalf, v, once);
+                        k += step;
+                        v += step;
                     }
                     continue;
                 }
+                // the page is that of any position that counts; positions before it on the page may not count, but lie there
+                const int one = half ? __ffs(half) - 1 : 0;
+                const long long from = __shfl_sync(0xffffffffu, at, 16 * b + one) - (half ? one * p.token_stride : 0) + my_at;
+                const char *k = static_cast<const char*>(p.k) + from, *v = static_cast<const char*>(p.v) + from;
 #pragma unroll
                 for (int i = 0; i < 16 / kRowsACopy; ++i) {
-                    const int row = i * kRowsACopy + my_row;
-                    const bool there = wanted && ((half >> row) & 1u);
-                    const uint32_t to = dst + G::piece(16 * b + row, my_piece);
-                    copy16(to, there ? k : p.k, there, once);
-                    copy16(to + G::kHalf, there ? v : p.v, there, once);
-                    k += kRowsACopy * p.token_stride;
-                    v += kRowsACopy * p.token_stride;
+                    const bool there = wanted && ((half >> (i * kRowsACopy + my_row)) & 1u);
+                    const uint32_t place = (to ^ G::piece(i * kRowsACopy, 0) % G::kRow) + i * kRowsACopy * G::kRow;
+                    copy16(place, there ? k : p.k, there, once);
+                    copy16(place + G::kHalf, there ? v : p.v, there, once);
+                    k += step;
+                    v += step;
                 }
             }
         } else {
@@ -925,8 +916,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 const int idx = 32 * i + lane, row = idx / G::kPieces, c = idx % G::kPieces;
                 const long long from = __shfl_sync(0xffffffffu, at, row) + 16 * c;
                 const bool there = ((who >> row) & 1u) && 16 * c < p.dh * kBytes;
-                copy16(dst + G::piece(row, c), there ? t.keys + from : p.k, there, once);
-                copy16(dst + G::kHalf + G::piece(row, c), there ? t.values + from : p.v, there, once);
+                copy16(dst + G::piece(row, c), there ? static_cast<const char*>(p.k) + from : p.k, there, once);
+                copy16(dst + G::kHalf + G::piece(row, c), there ? static_cast<const char*>(p.v) + from : p.v, there, once);
             }
         }
     };
@@ -1106,6 +1097,7 @@ int launch_as(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
     const long long units = (long long)p.kv_heads * ceil_div(p.group, p.heads_a_unit);
     if (units > INT_MAX) return GELO_ERR_UNSUPPORTED;
     p.units = (int)units;
+    p.units_a_kv = ceil_div(p.group, p.heads_a_unit);
     p.slot = 32 + p.heads_a_unit * p.dh;                      // a multiple of 8
     auto kernel = attend_kernel<T, W, kBytes>;
     // once per device: the attribute stays (asking again costs the host a microsecond)
