@@ -22,31 +22,59 @@ struct NormArgs {
     float eps;
 };
 
-// Sum and maximum over the kThreads threads that share a row
-template <int kThreads>
-__device__ __forceinline__ void row_reduce(float& sum, float& top)
+// Sum (in S) and maximum over the kThreads threads that share a row
+template <int kThreads, typename S>
+__device__ __forceinline__ S row_reduce(S sum, float& top)
 {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
         sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        if (sizeof(S) == 8) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     }
     if constexpr (kThreads > 32) {
-        __shared__ float2 part[kThreads / 32];
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(sum, top);
+        __shared__ S sums[kThreads / 32];
+        __shared__ float tops[kThreads / 32];
+        if ((threadIdx.x & 31) == 0) {
+            sums[threadIdx.x >> 5] = sum;
+            tops[threadIdx.x >> 5] = top;
+        }
         __syncthreads();
-        sum = 0.0f;
+        sum = 0;
 #pragma unroll
         for (int i = 0; i < kThreads / 32; ++i) {
-            sum += part[i].x;
-            top = fmaxf(top, part[i].y);
+            sum += sums[i];
+            if (sizeof(S) == 8) top = fmaxf(top, tops[i]);
         }
     }
+    return sum;
+}
+
+// Eight values times hi + lo as E4M3 codes of the exact products: where one rounds to the very middle of two codes, what the rounding has left decides.
+// (Rows of 16-bit values hold such products by the dozen: their quotients by the largest are short fractions.)
+__device__ __forceinline__ uint2 codes_of(const float (&v)[8], float hi, float lo)
+{
+    constexpr uint32_t kBelow = 0x7ffffu;                     // a middle has five significant bits: these are zero
+    float q[8];
+    bool middle = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        q[j] = fmaf(v[j], hi, v[j] * lo);
+        middle |= (__float_as_uint(q[j]) & kBelow) == 0;
+    }
+    if (middle) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float left = fmaf(v[j], lo, fmaf(v[j], hi, -q[j]));
+            const int bits = __float_as_int(q[j]);
+            if ((bits & kBelow) == 0 && left != 0.0f && q[j] != 0.0f) q[j] = __int_as_float(bits + (((__float_as_int(left) ^ bits) >> 31) | 1));
+        }
+    }
+    return e4m3_codes(q);
 }
 
 // kVecs groups of eight values per thread stay in registers; kVecs = 0: any width, the row is read a second time (from L2).
 // kThreads = 32: four rows per CTA, a warp each.
-template <typename T, int kThreads, int kVecs>
+template <typename T, int kThreads, int kVecs, bool kCodes>
 __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kernel(const NormArgs p)
 {
     chain_next();
@@ -61,6 +89,7 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
     constexpr int kKept = kVecs ? kVecs : 1;
     float h[kKept][8];
     float sum = 0.0f, top = 0.0f;
+    double sum64 = 0.0;
 
     auto load = [&](int g, float (&v)[8]) {
         Eight<T> a, b;
@@ -92,10 +121,18 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
         a.store(static_cast<T*>(to) + (size_t)row * ld + 8 * g);
     };
     auto collect = [&](int g, float (&v)[8]) {                // leaves h w in v
+        if constexpr (kCodes) {                                        // fp32 for four squares, binary64 beyond: the middles of codes hang on it (codes_of)
+            float four[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
+            for (int j = 0; j < 8; ++j) four[j >> 2] = fmaf(v[j], v[j], four[j >> 2]);
+            sum64 += (double)four[0];
+            sum64 += (double)four[1];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
+        }
         weigh(g, v);
-        if (p.codes) {
+        if constexpr (kCodes) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
         }
@@ -118,24 +155,26 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
             collect(g, h[0]);
         }
     }
-    row_reduce<kThreads>(sum, top);
-    const float inv = rsqrtf(sum / (float)p.d + p.eps);
-    float scale = 1.0f, to_code = 1.0f;
-    if (p.codes) {
-        const float s = __fdiv_rn(top * inv, 448.0f);
+    float inv, to_code = 0.0f, to_code_rest = 0.0f;
+    if constexpr (kCodes) {
+        // the row's scale and the factor of its codes in binary64, the factor as two floats
+        const double squares = row_reduce<kThreads>(sum64, top), inv64 = 1.0 / sqrt(squares / p.d + (double)p.eps);
+        float scale = 1.0f;
+        const float s = (float)((double)top * inv64 / 448.0);
         if (s > 0.0f) scale = s;
-        to_code = fminf(__fdiv_rn(inv, scale), FLT_MAX);      // a zero stays zero where the scale is next to nothing
-        if (!(sum <= FLT_MAX)) scale = to_code = __int_as_float(0x7fffffff);   // fmaxf passed over a NaN
+        const double f = fmin(inv64 / (double)scale, (double)FLT_MAX);             // a zero stays zero where the scale is next to nothing
+        to_code = (float)f;
+        to_code_rest = (float)(f - (double)to_code);
+        if (!(squares <= FLT_MAX)) scale = to_code = __int_as_float(0x7fffffff);      // fmaxf passed over a NaN
         if (t == 0) p.row_scale[row] = scale;
+        inv = (float)inv64;
+    } else {
+        inv = rsqrtf(row_reduce<kThreads>(sum, top) / (float)p.d + p.eps);
     }
 
     auto emit = [&](int g, float (&v)[8]) {                   // v: h w
         if (p.y) store(p.y, p.ldy, g, v, inv);
-        if (p.codes) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= to_code;
-            *reinterpret_cast<uint2*>(p.codes + (size_t)row * p.ldc + 8 * g) = e4m3_codes(v);
-        }
+        if constexpr (kCodes) *reinterpret_cast<uint2*>(p.codes + (size_t)row * p.ldc + 8 * g) = codes_of(v, to_code, to_code_rest);
     };
     if constexpr (kVecs > 0) {
 #pragma unroll
@@ -155,7 +194,8 @@ template <typename T, int kThreads, int kVecs>
 int launch_as(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
 {
     const int grid = kThreads == 32 ? ceil_div(p.rows, 4) : p.rows;
-    GELO_TRY(launch_chained(ctx, rms_norm_kernel<T, kThreads, kVecs>, dim3(grid), kThreads == 32 ? 128 : kThreads, 0, st, p));
+    GELO_TRY(launch_chained(ctx, p.codes ? rms_norm_kernel<T, kThreads, kVecs, true> : rms_norm_kernel<T, kThreads, kVecs, false>, dim3(grid),
+                            kThreads == 32 ? 128 : kThreads, 0, st, p));
     return after_launch(ctx);
 }
 

@@ -554,6 +554,28 @@ def test_captured_step_replays_on_new_inputs(ctx, cache):
     assert ctx.last_status() == binding.OK
 
 
+def test_first_calls_of_a_context_can_be_captured():
+    """No call before the capture: nothing that a kernel's first use does is forbidden there."""
+    c = binding.Context(0)
+    c.ensure_attention_workspace()
+    lens = [90, 7, 0]
+    paged, _ = filled(33, lens, 16, 1, 144, "token", "f16")
+    Q, x = rnd(90, 3, 5 * 144, dtype="f16"), rnd(91, 3, 720, dtype="f16")
+    o, y, ln = torch.zeros_like(Q), torch.empty_like(x), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    pos = torch.tensor([3, 4, -1], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.rms_norm(x, y)
+        c.append_kv(paged, y[:, :144], y[:, 144:288], pos)
+        c.paged_attention(paged, Q, ln, o)
+    graph.replay()
+    again = torch.empty_like(o)
+    c.paged_attention(paged, Q, ln, again)
+    assert torch.equal(o, again) and (o[2] == 0).all() and c.last_status() == binding.OK
+    c.close()
+
+
 def test_attention_on_two_streams_with_contexts_of_their_own():
     """Calls that may overlap on the GPU: each context has its own workspace."""
     ctxs = [binding.Context(0) for _ in range(2)]
