@@ -1,8 +1,8 @@
 // Root-mean-square norm with the residual's addition, and an output in E4M3 with a scale per row.
 //   h = x + r,  y = h (mean h^2 + eps)^-1/2 w,  scale = max|y| / 448,  code = E4M3(y / scale)
 // The maximum of |y| is that of |h w| times the row's factor, so one pass over the row collects the sum of squares and the maximum, with
-// the row in registers; the second half writes from there.  Bound by HBM: x and r in, h and y out.  4096 x 4096 bf16, 134 MB: 24.1 us, 86% of a copy's rate;
-// 1075 rows to E4M3 6.7 us (71%); 64 rows 2.7 us.
+// the row in registers; the second half writes from there.  Bound by HBM: x and r in, h and y out.  4096 x 4096 bf16, 134 MB: 22.8 us, 90% of a copy's rate
+// (8192 wide 43 us, 95%); 1075 rows to E4M3 7.2 us (66%: what decides a code on the right side of a middle takes the rest); 64 rows 2.7 us.
 #include <float.h>
 
 #include "common.cuh"
@@ -155,19 +155,32 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
             collect(g, h[0]);
         }
     }
-    float inv, to_code = 0.0f, to_code_rest = 0.0f;
+    float inv = 0.0f, to_code = 0.0f, to_code_rest = 0.0f;
     if constexpr (kCodes) {
-        // the row's scale and the factor of its codes in binary64, the factor as two floats
-        const double squares = row_reduce<kThreads>(sum64, top), inv64 = 1.0 / sqrt(squares / p.d + (double)p.eps);
-        float scale = 1.0f;
-        const float s = (float)((double)top * inv64 / 448.0);
-        if (s > 0.0f) scale = s;
-        const double f = fmin(inv64 / (double)scale, (double)FLT_MAX);             // a zero stays zero where the scale is next to nothing
-        to_code = (float)f;
-        to_code_rest = (float)(f - (double)to_code);
-        if (!(squares <= FLT_MAX)) scale = to_code = __int_as_float(0x7fffffff);      // fmaxf passed over a NaN
-        if (t == 0) p.row_scale[row] = scale;
-        inv = (float)inv64;
+        // the row's scale and the factor of its codes in binary64, the factor as two floats; a warp works them out for all
+        const double squares = row_reduce<kThreads>(sum64, top);
+        __shared__ float of_row[3];
+        if (t < 32) {
+            const double inv64 = rsqrt(squares / p.d + (double)p.eps);
+            float scale = 1.0f;
+            const float s = (float)((double)top * inv64 * (1.0 / 448.0));
+            if (s > 0.0f) scale = s;
+            const double f = fmin(inv64 / (double)scale, (double)FLT_MAX);         // a zero stays zero where the scale is next to nothing
+            to_code = (float)f;
+            to_code_rest = (float)(f - (double)to_code);
+            if (!(squares <= FLT_MAX)) scale = to_code = __int_as_float(0x7fffffff);  // fmaxf passed over a NaN
+            inv = (float)inv64;
+            if (t == 0) {
+                p.row_scale[row] = scale;
+                if (kThreads > 32) { of_row[0] = inv; of_row[1] = to_code; of_row[2] = to_code_rest; }
+            }
+        }
+        if (kThreads > 32) {
+            __syncthreads();
+            inv = of_row[0];
+            to_code = of_row[1];
+            to_code_rest = of_row[2];
+        }
     } else {
         inv = rsqrtf(row_reduce<kThreads>(sum, top) / (float)p.d + p.eps);
     }
@@ -190,30 +203,44 @@ __global__ void __launch_bounds__(kThreads == 32 ? 128 : kThreads) rms_norm_kern
     }
 }
 
-template <typename T, int kThreads, int kVecs>
+template <typename T, int kThreads, int kVecs, bool kCodes>
 int launch_as(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
 {
     const int grid = kThreads == 32 ? ceil_div(p.rows, 4) : p.rows;
-    GELO_TRY(launch_chained(ctx, p.codes ? rms_norm_kernel<T, kThreads, kVecs, true> : rms_norm_kernel<T, kThreads, kVecs, false>, dim3(grid),
-                            kThreads == 32 ? 128 : kThreads, 0, st, p));
+    GELO_TRY(launch_chained(ctx, rms_norm_kernel<T, kThreads, kVecs, kCodes>, dim3(grid), kThreads == 32 ? 128 : kThreads, 0, st, p));
     return after_launch(ctx);
 }
 
-template <typename T>
+template <typename T, bool kCodes>
 int launch_typed(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
 {
     // A warp a row up to 512 values; then as many threads as leave each one or two groups, since a row waits for its slowest thread and more
-    // threads in flight read more (4096 rows of 4096 bf16: 256 threads of two groups 24.2 us, 128 of four 26.5, 64 of eight 33, 512 of one 24.8;
-    // of 8192: 512 of two 46, 256 of four 49; of 2048: 256 of one 12.8, 128 of two 13.1).
-    const int groups = p.d / 8;
-    if (groups <= 32) return launch_as<T, 32, 1>(ctx, p, st);
-    if (groups <= 64) return launch_as<T, 32, 2>(ctx, p, st);
-    if (groups <= 128) return launch_as<T, 128, 1>(ctx, p, st);
-    if (groups <= 256) return launch_as<T, 256, 1>(ctx, p, st);
-    if (groups <= 512) return launch_as<T, 256, 2>(ctx, p, st);
-    if (groups <= 1024) return launch_as<T, 512, 2>(ctx, p, st);
-    if (groups <= 2048) return launch_as<T, 512, 4>(ctx, p, st);
-    return launch_as<T, 512, 0>(ctx, p, st);
+    // threads in flight read more (4096 rows of 4096 bf16: 256 threads of two groups 22.8 us, 128 of four 24.6, 512 of one 22.9;
+    // of 8192: 512 of two 43, 256 of four 46, 1024 of one 48).
+    // Rows with codes wait longer between their two halves, so half as many threads, and twice the rows per SM, where the rows are more than
+    // a wave of wide ones (five CTAs of 256 threads per SM, two of 512): 1000 rows of 2048 4.8 us against 5.3 with the wide shape, of 8192 16.5 against 18.5, 4096 rows 51.6
+    // against 60; few rows the other way, 148 of 2048 3.3 against 2.8, of 8192 4.8 against 4.1.  The thin shape of 4096 needs so many registers that
+    // it gains only where its wave of 8 per SM takes all: 1075 rows 7.2 against 8.0, 1480 rows 13.0 against 10.6, 4096 rows 28.3 against 27.5.
+    const int groups = p.d / 8, per_sm = ceil_div(p.rows, ctx->sm_count);
+    if (groups <= 32) return launch_as<T, 32, 1, kCodes>(ctx, p, st);
+    if (groups <= 64) return launch_as<T, 32, 2, kCodes>(ctx, p, st);
+    if (groups <= 128) return launch_as<T, 128, 1, kCodes>(ctx, p, st);
+    if constexpr (kCodes) {
+        if (groups <= 256 && per_sm > 5) return launch_as<T, 128, 2, true>(ctx, p, st);
+        if (groups > 256 && groups <= 512 && per_sm > 5 && per_sm <= 8) return launch_as<T, 128, 4, true>(ctx, p, st);
+        if (groups > 512 && groups <= 1024 && per_sm > 2) return launch_as<T, 256, 4, true>(ctx, p, st);
+    }
+    if (groups <= 256) return launch_as<T, 256, 1, kCodes>(ctx, p, st);
+    if (groups <= 512) return launch_as<T, 256, 2, kCodes>(ctx, p, st);
+    if (groups <= 1024) return launch_as<T, 512, 2, kCodes>(ctx, p, st);
+    if (groups <= 2048) return launch_as<T, 512, 4, kCodes>(ctx, p, st);
+    return launch_as<T, 512, 0, kCodes>(ctx, p, st);
+}
+
+template <typename T>
+int launch_codes_or_not(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
+{
+    return p.codes ? launch_typed<T, true>(ctx, p, st) : launch_typed<T, false>(ctx, p, st);
 }
 
 }  // namespace
@@ -226,9 +253,9 @@ int launch_rms_norm(gelo_ctx* ctx, const void* x, int ldx, const void* r, int ld
     p.codes = static_cast<uint8_t*>(codes); p.row_scale = row_scale;
     p.ldx = ldx; p.ldr = ldr; p.ldro = ldro; p.ldy = ldy; p.ldc = ldc;
     p.rows = rows; p.d = d; p.eps = eps;
-    if (dtype == GELO_BF16) return launch_typed<__nv_bfloat16>(ctx, p, st);
-    if (dtype == GELO_F16) return launch_typed<__half>(ctx, p, st);
-    return launch_typed<float>(ctx, p, st);
+    if (dtype == GELO_BF16) return launch_codes_or_not<__nv_bfloat16>(ctx, p, st);
+    if (dtype == GELO_F16) return launch_codes_or_not<__half>(ctx, p, st);
+    return launch_codes_or_not<float>(ctx, p, st);
 }
 
 }  // namespace gelo

@@ -64,7 +64,7 @@ def test_norm(ctx, dt, rows, d):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,d", [(1, 16), (66, 256), (5, 4096), (130, 1040), (2, 20000)])
+@pytest.mark.parametrize("rows,d", [(1, 16), (66, 256), (5, 4096), (130, 1040), (2, 20000), (1100, 1104), (1000, 4096), (1300, 4096), (400, 8192)])
 def test_norm_codes(ctx, dt, rows, d):
     x, r, w = rnd(4, rows, d, dtype=dt), rnd(5, rows, d, dtype=dt), (1 + 0.2 * rnd(6, d)).to(DT[dt])
     if rows > 1:
