@@ -360,7 +360,7 @@ int gelo_qkv_offload_blockdiag_batch(gelo_ctx* ctx, int calls, const void* const
  *
  * What a decoder layer does right before and right after the Q/K/V projection; the paper leaves these steps on the trusted side
  * (Section 3.2 offloads the projection only).  Rows of X, R, Y, Q, K, V and O may lie further apart than their width: a row stride is given
- * in elements and is a multiple of 8 (16 for codes).  Sums, norms and softmax statistics are held in fp32; every result is
+ * in elements and is a multiple of 8 (16 for codes).  Sums, norms and softmax statistics are held in fp32 or more; every result is
  * rounded once, to the type it is stored in.  The calls wait for nothing and can be captured into a graph; a graph keeps using the
  * workspace that was set when it was captured. */
 

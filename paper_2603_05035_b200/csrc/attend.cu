@@ -49,7 +49,7 @@ struct AttendArgs {
     const void *q, *k, *v;
     void* o;
     float *lse, *slots;
-    int* arrived;                                             // one counter per CTA, zero between calls
+    unsigned* arrived;                                             // one counter per CTA, zero between calls
     const int *len, *table;
     int* status;
     long long page_stride, token_stride, head_stride;         // bytes
@@ -1020,8 +1020,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         if (lane < 2) {
             const Cut c = lane ? cuts[1] : cuts[0];
             if (c.heads > 0) {
-                mine = atomicAdd(p.arrived + c.first, 1) == c.last - c.first;
-                if (mine) p.arrived[c.first] = 0;
+                const unsigned others = c.last - c.first;
+                mine = atomicInc(p.arrived + c.first, others) == others;              // (the last one leaves a zero)
             }
             last[lane] = mine;
         }

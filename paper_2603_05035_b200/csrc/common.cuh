@@ -53,7 +53,7 @@ struct gelo_ctx {
     size_t ws_bytes = 0;
     int* status_dev = nullptr;
     int* status_host = nullptr;   // pinned mirror
-    int* attend_arrived = nullptr;   // counters of the attention's CTAs, zero between calls (attend.cu)
+    unsigned* attend_arrived = nullptr;   // counters of the attention's CTAs, zero between calls (attend.cu)
     float gamma = 0.5f;
     float cond_bound = 100.0f;
     int max_attempts = 8;
