@@ -34,13 +34,14 @@ constexpr int kMaxCtas = 320;
 //   kWholeFew      the same where every head finds a CTA: 23 windows of 500 with 16 heads on one 24.3, whole 17.7
 //   kAloneCost     (two heads per CTA or more, all short) warps take heads of their own: 64 x 32 heads of up to 200 67, 22.5
 //   kLeast         tiles a warp gets where heads are cut: one sequence of 4000 x 4 heads 14.2 with four, 12.0 with two
-//   kMaxParts      one sequence of 32768, two key-value heads: 49 with 64 parts, 43 with 32, 38 with 48; of 8000 36, 24, 23
+//   kAtOnce        one sequence of 32768, four key-value heads (74 parts each of 8 heads): in one go 27.6, in rounds 24.5; eight (37 of 4) 31.3, 32.1
+//   kRound         the same with two (148 parts of 16 heads), rounds of 8 30.9, of 12 27.4, of 16 28.0; in one go with no more than 40 parts 37
 //   equal pieces   (few sequences; kPieceSlack) five of up to 4000 x 4 heads 14.4, in pieces 11.0; one of 32768 87.8, 86.0
 constexpr int kLeast = 2;                                     // tiles that a warp takes where heads are cut
 constexpr int kWhole = 24, kWholeFew = 56;                     // up to so many tiles a head stays in one piece; with no more heads than CTAs
 constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
 constexpr int kPieceSlack = 16;                               // equal pieces may be larger than a share by this part of it (or four tiles)
-constexpr int kMaxParts = 40;                                 // a head's sums come from no more than about so many CTAs
+constexpr int kAtOnce = 40, kRound = 12;                      // parts of a head that one CTA adds up in one go, or else in a round
 constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
 constexpr float kNone = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -49,7 +50,7 @@ struct AttendArgs {
     const void *q, *k, *v;
     void* o;
     float *lse, *slots;
-    unsigned* arrived;                                             // one counter per CTA, zero between calls
+    unsigned* arrived;                                        // two counters per CTA, zero between calls
     const int *len, *table;
     int* status;
     long long page_stride, token_stride, head_stride;         // bytes
@@ -697,6 +698,25 @@ __device__ __forceinline__ void add_part(float& top, float& total, float4& sum, 
 // A head that this CTA shares with others: those are CTAs first .. last, which leave their sums in slots
 struct Cut { int first, last, seq, head, heads; };
 
+// The parts of a head that are added up by one CTA: those of CTAs first, first + step .. last.  Up to kAtOnce parts in a single round; more in two, a
+// round of kRound neighbours, whose sums go to the slot of the first of them, and then the rounds.
+struct Round { int first, last, step; bool ends; };
+
+__device__ __forceinline__ Round round_of(const Cut& u, int level, int cta)
+{
+    const int after = u.last - u.first;
+    if (after < kAtOnce) return {u.first, u.last, 1, true};
+    if (level > 0) return {u.first, u.first + after / kRound * kRound, kRound, true};
+    const int first = u.first + (cta - u.first) / kRound * kRound;
+    return {first, min(first + kRound - 1, u.last), 1, false};
+}
+
+// Where CTA b leaves its part of a head that begins in CTA `first`: the second slot for the head that begins in b
+__device__ __forceinline__ float* slot_of(const AttendArgs& p, int b, int first)
+{
+    return p.slots + (size_t)(2 * b + (b == first ? 1 : 0)) * p.slot;
+}
+
 template <typename T, typename W, int kBytes>
 __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(const AttendArgs p)
 {
@@ -764,10 +784,9 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     const long long total = (all + (long long)cost * p.seqs) * p.units;
     long long share = quotient(total + gridDim.x * (alone ? kWarps : 1) - 1, gridDim.x * (alone ? kWarps : 1));
     if (!whole) {
-        // kLeast tiles for every warp, or an average head, since what a cut costs is more; and no head in many more than kMaxParts pieces
-        // (any share that is large enough will do: no division)
+        // kLeast tiles for every warp, or an average head, since what a cut costs is more (any share that is large enough will do: no division)
         const float average = (float)all * p.a_seq;
-        share = max(share, (long long)fmaxf(fminf((float)(kLeast * kWarps), average), average * (1.0f / kMaxParts)) + 1 + cost);
+        share = max(share, (long long)fminf((float)(kLeast * kWarps), average) + 1 + cost);
     }
     // Few sequences: their heads in equal pieces, one for a CTA, if pieces not much larger than a share find a CTA each.  No CTA then has
     // the end of one head and the beginning of another to see to.
@@ -775,7 +794,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     Walk<kTile> ahead, walk;
     if (!whole && few && heads_in_all <= (long long)gridDim.x) {
         const int grid = (int)gridDim.x, units = p.units, even = (int)fminf((float)(all * units) * p.a_cta, (float)(INT_MAX / 4)) + 1;
-        const int least = max(max(kLeast * kWarps, (longest + kMaxParts - 1) / kMaxParts), even), size = least + (int)((long long)least * lane / 32);
+        const int least = max(kLeast * kWarps, even), size = least + (int)((long long)least * lane / 32);
         int count = 0;                                        // pieces of this lane's size (the heads are as many as CTAs at most, so no sum gets far)
         const float a_piece = 1.0f / (float)size;
         for (int s = 0; s < p.seqs; ++s) count += min(pieces_of(__shfl_sync(0xffffffffu, n, s), size, a_piece), grid + 1);
@@ -978,7 +997,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         const long long unit_at = done.seq_at + (long long)done.unit * (n + cost) + cost;
         const int first_cta = in_one ? cta : piece_first >= 0 ? piece_first : (int)quotient(unit_at, share);
         const int last_cta = in_one ? cta : piece_first >= 0 ? piece_last : (int)quotient(unit_at + n - 1, share);
-        float* slot = p.slots + (size_t)(2 * cta + (first_cta == cta ? 1 : 0)) * p.slot;
+        float* const slot = slot_of(p, cta, first_cta);
         if (tid < done_heads) {
             const float total = all.total(tid);
             if (!in_one) {
@@ -1012,78 +1031,95 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
     }
 
     // ---- heads that several CTAs share, the first and the last of this one's at most: who arrives last adds up, in the order of the CTAs ----
-    if (cuts[0].heads + cuts[1].heads == 0) return;
-    __syncthreads();                                          // what the CTA's threads have written is before the first warp's fence ...
-    if (warp == 0) {
-        __threadfence();
-        bool mine = false;
-        if (lane < 2) {
-            const Cut c = lane ? cuts[1] : cuts[0];
-            if (c.heads > 0) {
-                const unsigned others = c.last - c.first;
-                mine = atomicInc(p.arrived + c.first, others) == others;              // (the last one leaves a zero)
-            }
-            last[lane] = mine;
-        }
-        __threadfence();                                      // ... and what other CTAs wrote before they arrived is before what follows the barrier
-    }
-    __syncthreads();
-    if (!last[0] && !last[1]) return;
 #pragma unroll 1
-    for (int k = 0; k < 2; ++k) {
-        if (!last[k]) continue;
-        const Cut u = k ? cuts[1] : cuts[0];
-        // a row of threads takes a head, or where there are more rows than heads every so-manieth part of one
-        const int together = min(u.heads, kRows), groups = kRows / together, group = my_h / together;
-        for (int h0 = 0; h0 < u.heads; h0 += together) {
-            const int h = h0 + my_h % together;
-            const bool works = group < groups && h < u.heads && c < p.dh;
-            float top = kNone, total = 0.0f;
-            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (works) {
-                constexpr int kBatch = 16;
-                for (int a = u.first + group; a <= u.last; a += kBatch * groups) {
-                    float2 t[kBatch];
-                    float4 v[kBatch];
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const int b = min(a + i * groups, u.last);
-                        const float* from = p.slots + (size_t)(2 * b + (b == u.first ? 1 : 0)) * p.slot;
-                        t[i] = *reinterpret_cast<const float2*>(from + 2 * h);
-                        v[i] = *reinterpret_cast<const float4*>(from + 32 + h * p.dh + c);
-                    }
-                    float higher = top;
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        if (a + i * groups > u.last) t[i] = make_float2(kNone, 0.0f);  // a part again: it weighs nothing (no branch, so that all loads fly at once)
-                        higher = fmaxf(higher, t[i].x);
-                    }
-                    add_part(top, total, sum, higher, top, total, sum, true);
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) add_part(top, total, sum, higher, t[i].x, t[i].y, v[i], false);
+    for (int level = 0; level < 2; ++level) {
+        if (cuts[0].heads + cuts[1].heads == 0) return;
+        __syncthreads();                                      // what the CTA's threads have written is before the first warp's fence ...
+        if (warp == 0) {
+            __threadfence();
+            if (lane < 2) {
+                const Cut u = lane ? cuts[1] : cuts[0];
+                bool mine = false;
+                if (u.heads > 0) {
+                    const Round r = round_of(u, level, cta);
+                    const unsigned others = (r.last - r.first) / r.step;
+                    // a round of few is counted at its last CTA: no other head has that one in its midst or as its end
+                    mine = atomicInc(p.arrived + (r.ends ? u.first : kMaxCtas + r.last), others) == others;        // (the last one leaves a zero)
                 }
+                last[lane] = mine;
             }
-            if (groups > 1) {                                 // (uniform)
-                float* const row = join + my_h * G::kJoinPitch;
-                __syncthreads();
+            __threadfence();                                  // ... and what other CTAs wrote before they arrived is before what follows the barrier
+        }
+        __syncthreads();
+        if (!last[0]) cuts[0].heads = 0;
+        if (!last[1]) cuts[1].heads = 0;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const Cut u = k ? cuts[1] : cuts[0];
+            if (u.heads == 0) continue;
+            const Round r = round_of(u, level, cta);
+            // a row of threads takes a head, or where there are more rows than heads every so-manieth part of one
+            const int together = min(u.heads, kRows), groups = kRows / together, group = my_h / together;
+            for (int h0 = 0; h0 < u.heads; h0 += together) {
+                const int h = h0 + my_h % together;
+                const bool works = group < groups && h < u.heads && c < p.dh;
+                float top = kNone, total = 0.0f;
+                float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (works) {
-                    *reinterpret_cast<float4*>(row + c) = sum;
-                    if (c == 0) { row[G::kWidth] = top; row[G::kWidth + 1] = total; }
+                    constexpr int kBatch = 16;
+                    for (int a = r.first + group * r.step; a <= r.last; a += kBatch * groups * r.step) {
+                        float2 t[kBatch];
+                        float4 v[kBatch];
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) {
+                            const float* from = slot_of(p, min(a + i * groups * r.step, r.last), u.first);
+                            t[i] = *reinterpret_cast<const float2*>(from + 2 * h);
+                            v[i] = *reinterpret_cast<const float4*>(from + 32 + h * p.dh + c);
+                        }
+                        float higher = top;
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) {
+                            if (a + i * groups * r.step > r.last) t[i] = make_float2(kNone, 0.0f);  // a part again: it weighs nothing (no branch, so that all loads fly at once)
+                            higher = fmaxf(higher, t[i].x);
+                        }
+                        add_part(top, total, sum, higher, top, total, sum, true);
+#pragma unroll
+                        for (int i = 0; i < kBatch; ++i) add_part(top, total, sum, higher, t[i].x, t[i].y, v[i], false);
+                    }
                 }
-                __syncthreads();
+                if (groups > 1) {                             // (uniform)
+                    float* const row = join + my_h * G::kJoinPitch;
+                    __syncthreads();
+                    if (works) {
+                        *reinterpret_cast<float4*>(row + c) = sum;
+                        if (c == 0) { row[G::kWidth] = top; row[G::kWidth + 1] = total; }
+                    }
+                    __syncthreads();
+                    if (works && group == 0) {
+                        float higher = kNone;
+                        for (int g = 0; g < groups; ++g) higher = fmaxf(higher, join[(my_h + g * together) * G::kJoinPitch + G::kWidth]);
+                        top = kNone;
+                        for (int g = 0; g < groups; ++g) {
+                            const float* const other = join + (my_h + g * together) * G::kJoinPitch;
+                            add_part(top, total, sum, higher, other[G::kWidth], other[G::kWidth + 1], *reinterpret_cast<const float4*>(other + c), g == 0);
+                        }
+                    }
+                }
+                if (!r.ends) __syncthreads();                 // (uniform) the slot that the sums go to has been read
                 if (works && group == 0) {
-                    float higher = kNone;
-                    for (int g = 0; g < groups; ++g) higher = fmaxf(higher, join[(my_h + g * together) * G::kJoinPitch + G::kWidth]);
-                    top = kNone;
-                    for (int g = 0; g < groups; ++g) {
-                        const float* const other = join + (my_h + g * together) * G::kJoinPitch;
-                        add_part(top, total, sum, higher, other[G::kWidth], other[G::kWidth + 1], *reinterpret_cast<const float4*>(other + c), g == 0);
+                    if (r.ends) {
+                        write_result<T>(p, u.seq, u.head + h, c, sum, total);
+                        if (p.lse && c == 0) p.lse[(size_t)u.seq * p.q_heads + u.head + h] = (top == kNone ? 0.0f : top * kLn2) + logf(total);
+                    } else {
+                        float* const to = slot_of(p, r.first, u.first);
+                        if (c == 0) *reinterpret_cast<float2*>(to + 2 * h) = make_float2(top, total);
+                        *reinterpret_cast<float4*>(to + 32 + h * p.dh + c) = sum;
                     }
                 }
             }
-            if (works && group == 0) {
-                write_result<T>(p, u.seq, u.head + h, c, sum, total);
-                if (p.lse && c == 0) p.lse[(size_t)u.seq * p.q_heads + u.head + h] = (top == kNone ? 0.0f : top * kLn2) + logf(total);
+            if (r.ends) {
+                if (k) cuts[1].heads = 0;
+                else cuts[0].heads = 0;
             }
         }
     }
@@ -1141,7 +1177,7 @@ int launch_fma(gelo_ctx* ctx, AttendArgs& p, cudaStream_t st)
 }  // namespace
 
 size_t attend_workspace_bytes() { return (size_t)2 * kMaxCtas * kSlotFloats * sizeof(float); }
-size_t attend_counter_bytes() { return kMaxCtas * sizeof(int); }
+size_t attend_counter_bytes() { return 2 * kMaxCtas * sizeof(unsigned); }
 
 int launch_paged_attention(gelo_ctx* ctx, const gelo_kv_cache& kv, const void* q, int ldq, int q_heads, const int* len, float scale, int window,
                            int dtype, void* o, int ldo, float* lse, void* ws, cudaStream_t st)

@@ -357,6 +357,17 @@ def test_attention_is_cut_along_the_length(ctx, dt, cache, lens, hq, hk):
 
 
 @pytest.mark.parametrize("dt,cache", TYPES)
+@pytest.mark.parametrize("lens,hq,hk,dh", [([21000], 1, 1, 128), ([21000], 32, 1, 64), ([30001], 16, 1, 256), ([9001, 20000], 3, 1, 96),
+                                           ([24000] + [5, 900, 0] * 13, 8, 2, 128), ([700] * 20 + [16000] + [300] * 20 + [16001], 2, 1, 64)])
+def test_attention_of_heads_in_many_parts(ctx, dt, cache, lens, hq, hk, dh):
+    """Heads cut over so many blocks that the sums are added up in rounds; with few sequences, and in the midst of many."""
+    paged, _ = filled(dh, lens, 32, hk, dh, "token", cache)
+    Q = rnd(49, len(lens), hq * dh, scale=2.0, dtype=dt)
+    check_attention(ctx, paged, Q, lens, dt, cache)
+    check_attention(ctx, paged, Q, lens, dt, cache, window=14000)
+
+
+@pytest.mark.parametrize("dt,cache", TYPES)
 def test_attention_with_one_key_that_counts(ctx, dt, cache):
     """Logits hundreds apart: the sums are rescaled on the way, and the weight of all others vanishes."""
     lens = [200, 37, 90]
