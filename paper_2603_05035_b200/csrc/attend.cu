@@ -235,7 +235,7 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 2^x for x <= 0, to two units in the last place; nothing where the result is no normal number
+// 2^x for x <= 14, to two units in the last place; nothing where the result is no normal number
 __device__ __forceinline__ float power2(float x)
 {
     float y;
@@ -310,6 +310,8 @@ struct MmaWarp {
     using G = Tiles<DH, kCodes ? 1 : 2>;
     static constexpr bool kPair = !(kCodes && std::is_same_v<T, __nv_bfloat16>);
     static constexpr int kHeads = 8 * NT;
+    // Halves have no exponents below 2^-24, where a long context's small weights are: p is kept relative to 2^-14 of the largest.
+    static constexpr float kRaise = 14.0f;
     uint32_t qf[DH / 16][NT][2];
     float acc[DH / 16][NT][4];
     float m[NT][2], l[NT][2], scale[NT][2];
@@ -441,6 +443,10 @@ struct MmaWarp {
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                if constexpr (std::is_same_v<M, __half>) {    // (where logits are so large that this rounds further down, p would leave a half's range)
+                    const float lower = top - kRaise;
+                    if (top - lower <= kRaise) top = lower;
+                }
                 top = fmaxf(top, m[n][j]);
                 const float base = top == kNone ? 0.0f : top;
                 keep[n][j] = power2(m[n][j] - base);

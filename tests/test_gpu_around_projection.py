@@ -368,6 +368,28 @@ def test_attention_of_heads_in_many_parts(ctx, dt, cache, lens, hq, hk, dh):
 
 
 @pytest.mark.parametrize("dt,cache", TYPES)
+@pytest.mark.parametrize("n", [400, 20000])
+def test_attention_of_many_small_weights(ctx, dt, cache, n):
+    """A key far above the others has a value of zero: what is left is the sum of weights of 2^-26 of the largest."""
+    paged, _ = filled(17, [n], 16, 1, 64, "token", cache)
+    at = torch.arange(n, device="cuda")
+    page = paged.table[0].long()[at // 16]
+    keys, vals = torch.zeros((n, 1, 64), device="cuda"), 0.5 + rnd(18, n, 1, 64).abs().clamp(max=2.0)
+    keys[n // 2, 0, 0] = 2.25
+    vals[n // 2] = 0
+    for x, new, f in ((paged.k, keys, 16), (paged.v, vals, 20)):
+        x[page, at % 16] = (new * f).to(torch.float8_e4m3fn).view(torch.uint8) if cache == "e4m3" else new.to(DT[cache])
+    Q = torch.zeros((1, 64), dtype=DT[dt], device="cuda")
+    Q[0, 0] = 8.0
+    ln, o, lse = torch.tensor([n], dtype=torch.int32, device="cuda"), torch.empty_like(Q), torch.empty((1, 1), device="cuda")
+    ctx.paged_attention(paged, Q, ln, o, scale=1.0, lse=lse)
+    ks, vs = paged.struct.k_scale, paged.struct.v_scale
+    o64, l64, weight, slack = ref.attend(Q.reshape(1, 1, 64), paged.k, paged.v, paged.table, [n], 1.0, 0, ks, vs)
+    tol_o, tol_l = ref.attend_tolerance(o64, l64, weight, slack, [n], 0.0, dt, cache)          # (nothing but errors relative to each weight)
+    assert ((o.reshape(1, 1, 64).double() - o64).abs() <= tol_o).all() and ((lse.double() - l64).abs() <= tol_l).all()
+
+
+@pytest.mark.parametrize("dt,cache", TYPES)
 def test_attention_with_one_key_that_counts(ctx, dt, cache):
     """Logits hundreds apart: the sums are rescaled on the way, and the weight of all others vanishes."""
     lens = [200, 37, 90]
