@@ -171,7 +171,7 @@ class Rope:
         _want(turns, "turns", torch.float64, 1)
         self.turns = turns if turns.is_contiguous() else turns.contiguous()
         self.struct = _RopeStruct(self.turns.data_ptr(), 2 * turns.numel(), 1 if interleaved else 0, magnitude)
-        self.ref = ctypes.addressof(self.struct)
+        self.ref, self.index, self.device = ctypes.addressof(self.struct), turns.get_device(), turns.device
 
 
 class PagedCache:
@@ -381,9 +381,9 @@ class Context:
                     "gelo_project_e4m3_rows")
 
     # ---- around the projection -------------------------------------------------------------
-    def _here(self, cache):
+    def _here(self, cache, name="the cache"):
         if cache.index != self.device:
-            raise ValueError(f"the cache is on {cache.device}, the context on cuda:{self.device}")
+            raise ValueError(f"{name} is on {cache.device}, the context on cuda:{self.device}")
 
     def rms_norm(self, X, Y=None, weight=None, eps=1e-5, residual=None, residual_out=None, codes=None, row_scale=None, stream=None):
         """Y = rms-normalised X + residual, times weight; residual_out = X + residual; codes and row_scale: the result in E4M3 (uint8 or
@@ -400,12 +400,15 @@ class Context:
 
     def rotary(self, X, heads, pos, rope, Y=None, stream=None):
         """Y (default: X itself) = X, n rows of `heads` heads, rotated to the positions pos (int32)."""
+        self._here(rope, "the rotation")
         self._check(_marshal.rotary(self._handle, self.device, X, heads, pos, rope.ref, Y, stream), "gelo_rotary")
 
     def append_kv(self, cache, K, V, pos, seq=None, rope=None, Q=None, Q_out=None, stream=None):
         """K (rotated) and V, n rows of kv_heads heads, go to position pos[i] of sequence seq[i] (default i); Q rotated goes to Q_out
         (default: Q itself)."""
         self._here(cache)
+        if rope is not None:
+            self._here(rope, "the rotation")
         self._check(_marshal.append_kv(self._handle, self.device, cache.ref, K, V, pos, seq, None if rope is None else rope.ref, Q, Q_out, stream),
                     "gelo_append_kv")
 

@@ -638,6 +638,42 @@ def test_attention_on_two_streams_with_contexts_of_their_own():
 
 # ---- refusals -------------------------------------------------------------------------------------------
 
+def test_two_graphs_share_a_workspace(ctx):
+    """Replayed in turn on one stream, with heads in many parts and in few."""
+    runs = []
+    for lens, hq, hk in (([20000], 4, 1), ([900, 0, 3000, 17], 8, 2)):
+        paged, _ = filled(hq, lens, 16, hk, 64, "token", "bf16")
+        Q, ln = rnd(50, len(lens), hq * 64, dtype="bf16"), torch.tensor(lens, dtype=torch.int32, device="cuda")
+        want, o = torch.empty_like(Q), torch.zeros_like(Q)
+        ctx.paged_attention(paged, Q, ln, want)
+        runs.append([paged, Q, ln, o, want, torch.cuda.CUDAGraph()])
+    torch.cuda.synchronize()
+    for paged, Q, ln, o, _, graph in runs:
+        with torch.cuda.graph(graph):
+            ctx.paged_attention(paged, Q, ln, o)
+    for turn in range(6):
+        for run in runs:
+            run[3].zero_()
+        for i in (0, 1, 1, 0)[turn % 3:]:
+            runs[i][5].replay()
+        torch.cuda.synchronize()
+        for i in set((0, 1, 1, 0)[turn % 3:]):
+            assert torch.equal(runs[i][3], runs[i][4])
+
+
+def test_rotation_of_another_device(ctx):
+    turns = torch.empty(32, dtype=torch.float64, device="cuda")
+    ctx.rope_turns(turns)
+    rope = binding.Rope(turns)
+    rope.index = 1                                             # as if the tensor were there
+    paged, _ = filled(1, [5], 4, 2, 64, "token", "bf16")
+    x, pos = rnd(51, 1, 128, dtype="bf16"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        ctx.rotary(x, 2, pos, rope)
+    with pytest.raises(ValueError):
+        ctx.append_kv(paged, x, x, pos, rope=rope)
+
+
 def test_refusals(ctx):
     x = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
     for kw in (dict(Y=None), dict(Y=x, row_scale=torch.zeros(4, device="cuda")), dict(Y=x, residual_out=x), dict(Y=x, eps=-1.0), dict(Y=x, eps=float("nan"))):
