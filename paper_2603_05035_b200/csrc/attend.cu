@@ -31,14 +31,15 @@ constexpr int kMaxCtas = 320;
 // How the line is dealt, with what either side of a choice takes (us; bf16 and heads of 128 unless said otherwise):
 //   kSegmentCost   weight of a head's beginning and end in tiles: 64 ragged sequences x 32 heads 343 without it, 309 with
 //   kWhole         heads this short are not cut: five fp32 sequences of up to 200 x 4 heads cut 15.4, whole 8.3
-//   kWholeFew      the same where every head finds a CTA: 23 windows of 500 with 16 heads on one 24.3, whole 17.7
+//   kWholeFew      the same where every head finds a CTA and equal pieces do not: 24 sequences of 440 x 8 heads cut 19.9, whole 13.3; of 880 24.4, 20.3
+//                  (24 sequences of 880 x 2 heads in pieces 13.6, whole 19.1; one of 440 x 4 9.4, 10.3)
 //   kAloneCost     (two heads per CTA or more, all short) warps take heads of their own: 64 x 32 heads of up to 200 67, 22.5
 //   kLeast         tiles a warp gets where heads are cut: one sequence of 4000 x 4 heads 14.2 with four, 12.0 with two
 //   kAtOnce        one sequence of 32768, four key-value heads (74 parts each of 8 heads): in one go 27.6, in rounds 24.5; eight (37 of 4) 31.3, 32.1
 //   kRound         the same with two (148 parts of 16 heads), rounds of 8 30.9, of 12 27.4, of 16 28.0; in one go with no more than 40 parts 37
 //   equal pieces   (few sequences; kPieceSlack) five of up to 4000 x 4 heads 14.4, in pieces 11.0; one of 32768 87.8, 86.0
 constexpr int kLeast = 2;                                     // tiles that a warp takes where heads are cut
-constexpr int kWhole = 24, kWholeFew = 56;                     // up to so many tiles a head stays in one piece; with no more heads than CTAs
+constexpr int kWhole = 24, kWholeFew = 56;                     // up to so many tiles a head stays in one piece; where it has a CTA but no two
 constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
 constexpr int kPieceSlack = 16;                               // equal pieces may be larger than a share by this part of it (or four tiles)
 constexpr int kAtOnce = 40, kRound = 12;                      // parts of a head that one CTA adds up in one go, or else in a round
@@ -785,7 +786,8 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
         }
     }
     const long long heads_in_all = (long long)p.seqs * p.units;
-    const bool whole = longest <= (heads_in_all <= gridDim.x ? kWholeFew : kWhole), alone = whole && heads_in_all >= 2 * (long long)gridDim.x;
+    const bool one_each = heads_in_all <= gridDim.x && !(few && 2 * heads_in_all <= gridDim.x);           // a CTA for a head, and no two equal pieces of it
+    const bool whole = longest <= (one_each ? kWholeFew : kWhole), alone = whole && heads_in_all >= 2 * (long long)gridDim.x;
     const int cost = alone ? kAloneCost : kSegmentCost, team = alone ? 1 : kWarps, member = alone ? 0 : warp;
     const long long total = (all + (long long)cost * p.seqs) * p.units;
     long long share = quotient(total + gridDim.x * (alone ? kWarps : 1) - 1, gridDim.x * (alone ? kWarps : 1));
