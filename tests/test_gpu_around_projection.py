@@ -367,6 +367,16 @@ def test_attention_of_heads_in_many_parts(ctx, dt, cache, lens, hq, hk, dh):
     check_attention(ctx, paged, Q, lens, dt, cache, window=14000)
 
 
+@pytest.mark.parametrize("dt,cache", TYPES[1:])
+@pytest.mark.parametrize("scale", [3e3, 1e6, 1e7, 3e8])
+def test_attention_of_huge_logits(ctx, dt, cache, scale):
+    """Logits whose neighbours in fp32 are further apart than the exponents of a half are wide: nothing overflows, one key takes all."""
+    lens = [300, 1, 4000, 33]
+    paged, _ = filled(19, lens, 16, 2, 64, "token", cache)
+    Q = rnd(52, 4, 6 * 64, scale=2.0, dtype=dt)
+    check_attention(ctx, paged, Q, lens, dt, cache, scale=scale)
+
+
 @pytest.mark.parametrize("dt,cache", TYPES)
 @pytest.mark.parametrize("n", [400, 20000])
 def test_attention_of_many_small_weights(ctx, dt, cache, n):
