@@ -36,13 +36,13 @@ constexpr int kMaxCtas = 320;
 //   kAloneCost     (two heads per CTA or more, all short) warps take heads of their own: 64 x 32 heads of up to 200 67, 22.5
 //   kLeast         tiles a warp gets where heads are cut: one sequence of 4000 x 4 heads 14.2 with four, 12.0 with two
 //   kAtOnce        one sequence of 32768, four key-value heads (74 parts each of 8 heads): in one go 27.6, in rounds 24.5; eight (37 of 4) 31.3, 32.1
-//   kRound         the same with two (148 parts of 16 heads), rounds of 8 30.9, of 12 27.4, of 16 28.0; in one go with no more than 40 parts 37
+//   kRound         the same with two (148 parts of 16 heads), rounds of 8 30.9, of 13 27.1, of 16 28.0; in one go with no more than 40 parts 37
 //   equal pieces   (few sequences; kPieceSlack) five of up to 4000 x 4 heads 14.4, in pieces 11.0; one of 32768 87.8, 86.0
 constexpr int kLeast = 2;                                     // tiles that a warp takes where heads are cut
 constexpr int kWhole = 24, kWholeFew = 56;                     // up to so many tiles a head stays in one piece; where it has a CTA but no two
 constexpr int kSegmentCost = 6, kAloneCost = 2;               // what a segment's beginning and end cost a CTA, and a warp alone, in tiles
 constexpr int kPieceSlack = 16;                               // equal pieces may be larger than a share by this part of it (or four tiles)
-constexpr int kAtOnce = 40, kRound = 12;                      // parts of a head that one CTA adds up in one go, or else in a round
+constexpr int kAtOnce = 40, kRound = 13;                      // parts of a head that one CTA adds up in one go, or else in a round
 constexpr int kSlotFloats = 16 * 256 + 32;                    // most that a slot holds: maxima and totals of 16 heads, their sums
 constexpr float kNone = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(32 * W::G::kWarps, W::G::kCtas) attend_kernel(
                 float top = kNone, total = 0.0f;
                 float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (works) {
-                    constexpr int kBatch = 16;
+                    constexpr int kBatch = kRound;
                     for (int a = r.first + group * r.step; a <= r.last; a += kBatch * groups * r.step) {
                         float2 t[kBatch];
                         float4 v[kBatch];
