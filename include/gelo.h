@@ -361,8 +361,8 @@ int gelo_qkv_offload_blockdiag_batch(gelo_ctx* ctx, int calls, const void* const
  * What a decoder layer does right before and right after the Q/K/V projection; the paper leaves these steps on the trusted side
  * (Section 3.2 offloads the projection only).  Rows of X, R, Y, Q, K, V and O may lie further apart than their width: a row stride is given
  * in elements and is a multiple of 8 (16 for codes).  Sums, norms and softmax statistics are held in fp32 or more; every result is
- * rounded once, to the type it is stored in.  The calls wait for nothing and can be captured into a graph; a graph keeps using the
- * workspace that was set when it was captured. */
+ * rounded once, to the type it is stored in.  The calls wait for nothing and can be captured into a graph; replays have to be ordered with
+ * the other calls of their context and end before it is destroyed. */
 
 /* Root-mean-square norm of `rows` rows of d values, with the residual's addition:
  *     h = X + R (R_dev may be NULL: h = X),  y = h / sqrt(mean(h^2) + eps) * weight  (weight_dev, d values, may be NULL: 1).
@@ -431,9 +431,15 @@ int gelo_append_kv(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* K_dev,
  * lse_dev (optional, seqs x q_heads floats): log sum_j exp(scale q . k_j).  A length of zero or less gives o = 0 and lse = -infinity.
  * Entries of the cache outside those positions are not read, or do not count whatever they hold.  A length beyond the table is cut to it, and a page
  * outside the cache counts as absent; both record GELO_ERR_INVALID.  A key whose logit is minus infinity does not count either; an infinity
- * among the values that count makes its component infinite or NaN.  Sequences may share pages.  The same inputs give the same bytes.  Needs a
- * workspace of gelo_attention_workspace_bytes() bytes, whatever the sizes. */
+ * among the values that count makes its component infinite or NaN.  Sequences may share pages.  The same inputs give the same bytes.
+ * Works in the buffer of gelo_set_attention_workspace.  Without one, a call that is not being captured works in that of gelo_set_workspace (at
+ * least gelo_attention_workspace_bytes()) and a captured one returns GELO_ERR_WORKSPACE: a batch of the context starts sampling into that
+ * buffer early, which a call holds back and a replay cannot. */
 size_t gelo_attention_workspace_bytes(void);
+/* Hands the context a caller-owned device buffer for gelo_paged_attention alone: 256-byte aligned, gelo_attention_workspace_bytes() bytes whatever the
+ * sizes of the calls (NULL, 0 takes it away).  It must stay valid until replaced or the context is destroyed, and as long as graphs replay that
+ * captured a call with it. */
+int gelo_set_attention_workspace(gelo_ctx* ctx, void* dev_ws, size_t bytes);
 int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* Q_dev, int ldq, int q_heads, const int* len_dev,
                          float scale, int window, int dtype, void* O_dev, int ldo, float* lse_dev, void* stream);
 

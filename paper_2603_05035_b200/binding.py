@@ -68,6 +68,7 @@ EXPORTS = {
     "gelo_rotary": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _i, _vp]),
     "gelo_append_kv": (_i, [_vp, _vp, _vp, _i, _vp, _i, _vp, _i, _i, _i, _vp, _vp, _vp, _i, _vp, _i, _vp]),
     "gelo_attention_workspace_bytes": (_sz, []),
+    "gelo_set_attention_workspace": (_i, [_vp, _vp, _sz]),
     "gelo_paged_attention": (_i, [_vp, _vp, _vp, _i, _i, _vp, _f, _i, _i, _vp, _i, _vp, _vp]),
     "gelo_qkv_offload": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _u64, _f, _i, _vp, _vp, _vp, _vp]),
     "gelo_project_unmix": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
@@ -219,6 +220,7 @@ class Context:
         self._h = h
         self._handle = h.value
         self._ws = None
+        self._attend_ws = None
 
     def close(self):
         if getattr(self, "_h", None):
@@ -413,10 +415,15 @@ class Context:
                     "gelo_append_kv")
 
     def ensure_attention_workspace(self):
-        """Allocates (with torch) a workspace large enough for paged_attention, if the current one is not."""
+        """Allocates (with torch) the scratch of paged_attention, if the context has none: memory of its own, kept for the context's lifetime, which
+        captured calls need."""
         need = int(self._lib.gelo_attention_workspace_bytes())
-        if self._ws is None or self._ws.numel() * self._ws.element_size() < need:
-            self.set_workspace(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
+        if self._attend_ws is None:
+            t = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream(self.device).synchronize()   # what used this memory before is over, whatever stream the calls come on
+            self._check(self._lib.gelo_set_attention_workspace(self._h, t.data_ptr(), need), "gelo_set_attention_workspace")
+            self._attend_ws = t
         return need
 
     def paged_attention(self, cache, Q, lengths, O, scale=None, window=0, lse=None, stream=None):

@@ -1453,6 +1453,14 @@ int gelo_append_kv(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* K_dev,
 
 size_t gelo_attention_workspace_bytes(void) { return attend_workspace_bytes(); }
 
+int gelo_set_attention_workspace(gelo_ctx* ctx, void* dev_ws, size_t bytes)
+{
+    if (!ctx || (reinterpret_cast<uintptr_t>(dev_ws) & 255u)) return GELO_ERR_INVALID;
+    if (dev_ws && bytes < attend_workspace_bytes()) return GELO_ERR_WORKSPACE;
+    ctx->attend_ws = dev_ws;
+    return GELO_OK;
+}
+
 int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* Q_dev, int ldq, int q_heads, const int* len_dev,
                          float scale, int window, int dtype, void* O_dev, int ldo, float* lse_dev, void* stream)
 {
@@ -1467,9 +1475,18 @@ int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* 
         (Q_dev == O_dev && ldq != ldo))
         return GELO_ERR_INVALID;
     DeviceGuard guard(ctx->device);
-    if (!ctx->ws || ctx->ws_bytes < attend_workspace_bytes()) return GELO_ERR_WORKSPACE;
-    ctx->chain_valid = false;      // a later batch must not sample into the workspace before this call is done with it
-    return launch_paged_attention(ctx, *cache, Q_dev, ldq, q_heads, len_dev, scale, window, dtype, O_dev, ldo, lse_dev, ctx->ws, as_stream(stream));
+    void* scratch = ctx->attend_ws;
+    if (!scratch) {
+        // The workspace that batches sample into, too: a later batch must not begin before this call is done with it.  A replay of a captured call could not
+        // see to that, as it runs nothing here.
+        if (!ctx->ws || ctx->ws_bytes < attend_workspace_bytes()) return GELO_ERR_WORKSPACE;
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        GELO_CUDA_OK(cudaStreamIsCapturing(as_stream(stream), &capture));
+        if (capture != cudaStreamCaptureStatusNone) return GELO_ERR_WORKSPACE;
+        ctx->chain_valid = false;
+        scratch = ctx->ws;
+    }
+    return launch_paged_attention(ctx, *cache, Q_dev, ldq, q_heads, len_dev, scale, window, dtype, O_dev, ldo, lse_dev, scratch, as_stream(stream));
 }
 
 int gelo_profile_start(gelo_ctx* ctx)

@@ -54,6 +54,7 @@ struct gelo_ctx {
     int* status_dev = nullptr;
     int* status_host = nullptr;   // pinned mirror
     unsigned* attend_arrived = nullptr;   // counters of the attention's CTAs, zero between calls (attend.cu)
+    void* attend_ws = nullptr;            // the attention's own scratch (gelo_set_attention_workspace)
     float gamma = 0.5f;
     float cond_bound = 100.0f;
     int max_attempts = 8;
