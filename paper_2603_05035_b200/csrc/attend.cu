@@ -15,6 +15,7 @@
 // the same in fp32 597 us (105%, reads alone run faster than a copy), E4M3 196 us (80%, bound by the widening of the codes); one sequence of 32768
 // bf16 86 us (96%); 8 of 32 heads on E4M3 111 us (90%).  Two CTAs of four warps per SM: with one of eight the end of a segment leaves the SM
 // idle (64 sequences 364 us against 345 at the time).
+#include <float.h>
 #include <limits.h>
 
 #include <atomic>
@@ -316,6 +317,7 @@ struct MmaWarp {
     uint32_t qf[DH / 16][NT][2];
     float acc[DH / 16][NT][4];
     float m[NT][2], l[NT][2], scale[NT][2];
+    bool may_vanish;                                          // a logit of this segment may be minus infinity (the same in all lanes)
 
     static constexpr int kStaged = 0;                         // floats of shared memory for a warp's q
 
@@ -347,6 +349,9 @@ struct MmaWarp {
     __device__ __forceinline__ void begin(const AttendArgs& p, float*, int lane)
     {
         const int t = lane & 3;
+        // Codes are finite and products with q in [-2, 2] bounded, so only an infinite q or a scale that overflows could do it, and nearly all segments are spared
+        // the look at their logits (33 long sequences, 8 of 32 heads, f16: 106.7 us, 110.8 with it); the elements of the other caches may be infinite.
+        bool vanish = !kCodes;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float factor = 1.0f;
@@ -360,6 +365,7 @@ struct MmaWarp {
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 int e = 0;
                 if (top > 0.0f && top <= 3.4e38f) e = max(ilogbf(top), -126);
+                vanish |= top > 3.4e38f;
                 factor = exp2f((float)e);
                 const float down = exp2f((float)-e);
 #pragma unroll
@@ -374,6 +380,7 @@ struct MmaWarp {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 scale[n][j] = p.scale * kLog2e * (kCodes ? __shfl_sync(0xffffffffu, factor, 4 * (2 * t + j)) : 1.0f);
+                if constexpr (kCodes) vanish |= !(fabsf(scale[n][j]) * (2.0f * 448.0f * DH) <= FLT_MAX);
                 m[n][j] = kNone;
                 l[n][j] = 0.0f;
             }
@@ -382,9 +389,18 @@ struct MmaWarp {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[s][n][j] = 0.0f;
         }
+        may_vanish = !kCodes || __any_sync(0xffffffffu, vanish);
     }
 
     __device__ __forceinline__ void tile(uint32_t keys, uint32_t values, uint32_t counts, int lane)
+    {
+        // (a tile of codes that is spared the look has code of its own: 105 us, 107 where it jumps over it; with two sets of heads the registers do not suffice for both)
+        if (kCodes && NT == 1 && !may_vanish) tile_as<false>(keys, values, counts, lane);
+        else tile_as<true>(keys, values, counts, lane);
+    }
+    // kLook: logits of minus infinity are looked for
+    template <bool kLook>
+    __device__ __forceinline__ void tile_as(uint32_t keys, uint32_t values, uint32_t counts, int lane)
     {
         constexpr int kSub = G::kTile / 16;
         const int r = lane >> 2;
@@ -421,6 +437,28 @@ struct MmaWarp {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma(c[b][n], a, qf[s][n][0], qf[s][n][1], M());
                 }
+            }
+        }
+        // A logit of minus infinity weighs nothing, but a product with its value would make a NaN of an infinity there.  Hardly any tile has one: `gone`
+        // then has a bit for each of this lane's logits.  (Zeros stand where no key is, so only keys that count are seen.)
+        bool any_gone = false;
+        uint32_t gone = 0;
+        if (kLook && (!kCodes || may_vanish)) {
+#pragma unroll
+            for (int b = 0; b < kSub; ++b)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) any_gone |= c[b][n][j] * scale[n][j & 1] == kNone;
+            any_gone = __any_sync(0xffffffffu, any_gone);
+            if (any_gone) {
+#pragma unroll
+                for (int i = 0; i < 2 * kSub; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (c[i >> 1][n][2 * (i & 1) + j] * scale[n][j] == kNone) gone |= 1u << (2 * (NT * i + n) + j);
             }
         }
         // positions of this lane: r + 8 i
@@ -479,6 +517,7 @@ struct MmaWarp {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[s][n][j] *= keep[n][j & 1];
         }
+        if (any_gone) pass_over(values, gone, ph, pl, lane);
         const int pos = (lane & 7) + ((lane >> 4) << 3), col = (lane >> 3) & 1;
 #pragma unroll
         for (int b = 0; b < kSub; ++b) {
@@ -512,6 +551,71 @@ struct MmaWarp {
                 }
             }
         }
+    }
+
+    // Positions with a logit of minus infinity for some head (a bit of `gone`, see tile): their values are added to the sums of the other heads one
+    // by one, and cleared before the products of the tile.
+    template <int kSub>
+    __device__ __forceinline__ void pass_over(uint32_t values, uint32_t gone, const uint32_t (&ph)[kSub][NT][2], const uint32_t (&pl)[kSub][NT][2], int lane)
+    {
+        const int r = lane >> 2, t = lane & 3;
+        constexpr uint32_t kOfRow = (1u << 2 * NT) - 1;
+        uint32_t rows = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * kSub; ++i) {
+            const uint32_t lanes = __ballot_sync(0xffffffffu, (gone >> (2 * NT * i)) & kOfRow);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) rows |= ((lanes >> (4 * u)) & 15u) ? 1u << (8 * i + u) : 0u;
+        }
+#pragma unroll 1
+        for (; rows; rows &= rows - 1) {
+            const int at = __ffs(rows) - 1, from = 4 * (at & 7) + t;              // lane `from` has the position's weights of this lane's heads
+            const uint32_t skip = __shfl_sync(0xffffffffu, gone, from) >> (2 * NT * (at >> 3));
+            float p[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                uint32_t high = 0, low = 0;
+#pragma unroll
+                for (int i = 0; i < 2 * kSub; ++i) {          // (masks: an index that the loop works out would put the arrays into local memory)
+                    const uint32_t its = i == at >> 3 ? 0xffffffffu : 0u;
+                    high |= ph[i >> 1][n][i & 1] & its;
+                    if constexpr (kPair) low |= pl[i >> 1][n][i & 1] & its;
+                }
+                high = __shfl_sync(0xffffffffu, transposed(high), from);
+                if constexpr (kPair) low = __shfl_sync(0xffffffffu, transposed(low), from);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    p[n][j] = widen_at(reinterpret_cast<const M*>(&high), j) + (kPair ? widen_at(reinterpret_cast<const M*>(&low), j) : 0.0f);
+            }
+#pragma unroll
+            for (int s = 0; s < DH / 16; ++s) {
+                float v[2];
+                if constexpr (kCodes) {
+                    uint16_t two;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(two) : "r"(values + G::piece(at, s) + 2 * r) : "memory");
+                    uint32_t x, unused;
+                    halves_of_codes(two, x, unused);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) v[j] = widen_at(reinterpret_cast<const M*>(&x), j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint16_t one;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(one) : "r"(values + G::piece(at, 2 * s + j) + 2 * r) : "memory");
+                        v[j] = widen_at(reinterpret_cast<const M*>(&one), 0);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (!((skip >> (2 * n + (j & 1))) & 1u)) acc[s][n][j] = fmaf(p[n][j & 1], v[j >> 1], acc[s][n][j]);
+            }
+            __syncwarp();
+            for (int i = lane; i < G::kPieces; i += 32)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(values + G::piece(at, i)), "r"(0u) : "memory");
+        }
+        __syncwarp();
     }
 
     // maxima and totals of heads [0, kHeads) into shared memory
@@ -609,11 +713,24 @@ struct FmaWarp {
             }
         }
         const bool on = (counts >> row) & 1u;
-        float e[H];
+        bool any_gone = false;                                // see MmaWarp::tile
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
-            s[h] = on ? s[h] * scale : kNone;
+            s[h] *= scale;
+            any_gone |= s[h] == kNone;
+        }
+        any_gone = __any_sync(0xffffffffu, any_gone);
+        uint32_t gone = 0;
+        if (any_gone) {
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+                if (s[h] == kNone) gone |= 1u << h;
+        }
+        float e[H];
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            s[h] = on ? s[h] : kNone;
             float top = s[h];
 #pragma unroll
             for (int off = 1; off < 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -625,6 +742,22 @@ struct FmaWarp {
             l[h] = fmaf(l[h], keep, side ? 0.0f : e[h]);
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) acc[h][i] *= keep;
+        }
+        if (any_gone) {
+#pragma unroll 1
+            for (int t = 0; t < G::kTile; ++t) {
+                float v[kOwn];
+                load_own(v, values, t, lane);
+                const uint32_t skip = __shfl_sync(0xffffffffu, gone, t);
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    const float w = __shfl_sync(0xffffffffu, e[h], t);
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i)
+                        if (!((skip >> h) & 1u)) acc[h][i] = fmaf(w, v[i], acc[h][i]);
+                }
+            }
+            return;
         }
 #pragma unroll 8
         for (int t = 0; t < G::kTile; ++t) {

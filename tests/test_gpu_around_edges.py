@@ -131,3 +131,131 @@ def test_attention_in_the_shared_workspace():
     torch.cuda.synchronize()
     assert torch.equal(o, want)
     c.close()
+
+
+# ---- keys whose logit is minus infinity ---------------------------------------------------------------
+
+def entries(lens, ps, paged):
+    """Page and place of every position of each sequence."""
+    out = []
+    for s, n in enumerate(lens):
+        t = torch.arange(n, device="cuda")
+        out.append((paged.table[s].long()[t // ps], t % ps))
+    return out
+
+
+def compacted(paged, where, keep):
+    """The positions of each sequence that `keep` leaves, as a cache of pages of one token: keys, values, table, lengths."""
+    most = max(int(k.sum()) for k in keep)
+    table = torch.full((len(keep), most + 1), -1, dtype=torch.int32, device="cuda")
+    ks, vs, at = [], [], 0
+    for s, ((page, place), on) in enumerate(zip(where, keep)):
+        n = int(on.sum())
+        table[s, :n] = torch.arange(at, at + n, dtype=torch.int32, device="cuda")
+        ks.append(paged.k[page[on], place[on]])
+        vs.append(paged.v[page[on], place[on]])
+        at += n
+    return torch.cat(ks)[:, None], torch.cat(vs)[:, None], table, [int(on.sum()) for on in keep]
+
+
+def attend_to(ctx, paged, Q, lens, dt):
+    o, lse = torch.full_like(Q, 7.0), torch.full((len(lens), Q.shape[1] // paged.head_dim), 7.0, device="cuda")
+    ctx.paged_attention(paged, Q, torch.tensor(lens, dtype=torch.int32, device="cuda"), o, lse=lse)
+    assert ctx.last_status() == binding.OK
+    return o.reshape(len(lens), -1, paged.head_dim).double(), lse.double()
+
+
+def assert_near(got, got_lse, want, lens, vmax, dt, cache, heads=slice(None)):
+    o64, l64, weight, slack = want
+    tol_o, tol_l = ref.attend_tolerance(o64, l64, weight, slack, [max(n, 1) for n in lens], vmax, dt, cache)
+    empty = torch.isinf(l64)
+    assert ((got - o64).abs() <= tol_o)[:, heads].all()
+    assert torch.equal(torch.isneginf(got_lse)[:, heads], empty[:, heads])
+    assert (((got_lse - l64).abs() <= tol_l) | empty)[:, heads].all()
+
+
+LENS = [[40, 5000, 17, 1], [(37 * i) % 23 + 1 for i in range(700)], [33] * 40]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lens", LENS, ids=["cut", "alone", "whole"])
+@pytest.mark.parametrize("hq,hk,dh", [(1, 1, 64), (8, 2, 128), (14, 1, 64), (12, 1, 256), (3, 1, 80)])
+def test_values_behind_keys_of_minus_infinity(ctx, dt, lens, hq, hk, dh):
+    """Keys of minus infinity, whole tiles of them too: their values do not count, be they infinite or NaN."""
+    ps = 8
+    paged, _ = filled(dh + hq, lens, ps, hk, dh, "token", dt)
+    where, keep = entries(lens, ps, paged), []
+    for s, (page, place) in enumerate(where):
+        t = torch.arange(lens[s], device="cuda")
+        gone = (t * t * 7 + s) % 5 == 0
+        gone |= (t >= 96) & (t < 160)
+        if s % 4 == 3:
+            gone |= True
+        keep.append(~gone)
+        paged.k[page[gone], place[gone], :, 0] = -math.inf
+        bad = torch.tensor([math.nan, math.inf, -math.inf], device="cuda").to(DT[dt])[t[gone] % 3]
+        paged.v[page[gone], place[gone]] = bad[:, None, None]
+    Q = rnd(80, len(lens), hq * dh, scale=2.0, dtype=dt)
+    Q.reshape(len(lens), hq, dh)[..., 0] = 0.75
+    got, lse = attend_to(ctx, paged, Q, lens, dt)
+    k, v, table, left = compacted(paged, where, keep)
+    want = ref.attend(Q.reshape(len(lens), hq, dh), k, v, table, left, dh ** -0.5)
+    assert torch.isfinite(got).all()
+    assert_near(got, lse, want, left, ref.values(v).abs().max(), dt, dt)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", LENS, ids=["cut", "alone", "whole"])
+@pytest.mark.parametrize("hq,dh", [(4, 64), (8, 128), (14, 64), (12, 256)])
+def test_keys_of_minus_infinity_for_some_heads(ctx, dt, lens, hq, dh):
+    """Keys so large that the logits of every other head overflow: those heads pass over the value, the others do not, and see an infinity in it."""
+    ps = 16
+    paged, _ = filled(dh + hq, lens, ps, 1, dh, "head", dt)
+    where, keep = entries(lens, ps, paged), []
+    for s, (page, place) in enumerate(where):
+        t = torch.arange(lens[s], device="cuda")
+        gone = (t * 11 + s) % 13 == 3
+        keep.append(~gone)
+        paged.k[page, place, :, 0] = 0.0
+        paged.v[page[gone], place[gone], :, 5] = math.inf
+    Q = rnd(81, len(lens), hq * dh, scale=2.0, dtype=dt)
+    q = Q.reshape(len(lens), hq, dh)
+    q[:, 0::2, 0] = 4.0
+    q[:, 1::2, 0] = 0.0
+    vmax = 8.0
+    k, v, table, left = compacted(paged, where, keep)
+    passed = ref.attend(q, k, v, table, left, dh ** -0.5)
+    counted = ref.attend(q, paged.k, paged.v, paged.table, lens, dh ** -0.5)
+    for (page, place), on in zip(where, keep):
+        paged.k[page[~on], place[~on], :, 0] = -3e38
+    got, lse = attend_to(ctx, paged, Q, lens, dt)
+    assert torch.isfinite(got[:, 0::2]).all()
+    assert_near(got, lse, passed, left, vmax, dt, dt, slice(0, None, 2))
+    some = torch.tensor([not bool(on.all()) for on in keep], device="cuda")
+    assert not torch.isfinite(got[some][:, 1::2, 5]).any()     # infinite, or NaN where a weight is too small for fp32
+    got[some, :, 5] = 0.0
+    for x in counted[0], counted[2]:
+        x[some, :, 5] = 0.0
+    assert_near(got, lse, counted, lens, vmax, dt, dt, slice(1, None, 2))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("lens", LENS, ids=["cut", "alone", "whole"])
+@pytest.mark.parametrize("hq,dh", [(2, 64), (8, 128), (14, 64), (12, 256)])
+def test_logits_of_minus_infinity_on_codes(ctx, dt, lens, hq, dh):
+    """A query of minus infinity makes every logit of its head one: that head is zero whatever the values hold, and sees none of its neighbours'."""
+    ps = 16
+    paged, scales = filled(dh + hq, lens, ps, 1, dh, "token", "e4m3")
+    for page, place in entries(lens, ps, paged):
+        paged.k[page, place, :, 0] = 0x38                      # one, before its scale
+    Q = rnd(82, len(lens), hq * dh, scale=2.0, dtype=dt)
+    q = Q.reshape(len(lens), hq, dh)
+    clean = ref.attend(q, paged.k, paged.v, paged.table, lens, dh ** -0.5, 0, *scales.values())
+    q[:, 0::2, 0] = -math.inf
+    got, lse = attend_to(ctx, paged, Q, lens, dt)
+    assert (got[:, 0::2] == 0).all() and torch.isneginf(lse[:, 0::2]).all()
+    assert_near(got, lse, clean, lens, 448 / 20, dt, "e4m3", slice(1, None, 2))
+    for page, place in entries(lens, ps, paged):
+        paged.v[page, place] = 0x7F
+    got, lse = attend_to(ctx, paged, Q, lens, dt)
+    assert (got[:, 0::2] == 0).all() and got[:, 1::2].isnan().all()
