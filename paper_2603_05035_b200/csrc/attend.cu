@@ -303,14 +303,14 @@ struct Joint {
 // ---- products of a warp on a 16-bit or E4M3 tile: mma.sync on transposed operands ---------------------------
 // S^T = K q^T and O^T = V^T p^T: positions (and components) are the 16 rows of an instruction, up to eight query heads its columns, so a
 // single head wastes columns of an otherwise idle unit and no loads.  The matrix rate that this leaves is several times what HBM
-// can feed (16 instructions per 8 KB tile of 128 components).  p is handed to the second product as the 16-bit value and what
-// that leaves out, i.e. with 16 bits, so the stored result is rounded once; E4M3 caches with bf16 results take it as one half (11 bits).
+// can feed (24 instructions per 8 KB tile of 128 components).  p is handed to the second product as the 16-bit value and what
+// that leaves out, i.e. with 16 bits (bf16 caches) or 22, so that the stored result is rounded once.  (E4M3 caches with bf16 results, p as one half of 11 bits: half
+// the second products; 33 long sequences, 8 of 32 heads 108 us as with both, 16 heads a key-value head 141 instead of 156; 5 times the distance from a form in fp32.)
 // E4M3 tiles are widened to half in registers, q is given the same type times a power of two that puts its largest component into [1, 2).
 template <typename T, bool kCodes, int DH, int NT>
 struct MmaWarp {
     using M = std::conditional_t<kCodes, __half, T>;
     using G = Tiles<DH, kCodes ? 1 : 2>;
-    static constexpr bool kPair = !(kCodes && std::is_same_v<T, __nv_bfloat16>);
     static constexpr int kHeads = 8 * NT;
     // Halves have no exponents below 2^-24, where a long context's small weights are: p is kept relative to 2^-14 of the largest.
     static constexpr float kRaise = 14.0f;
@@ -503,10 +503,8 @@ struct MmaWarp {
             for (int i = 0; i < 2 * kSub; ++i) {
                 const uint32_t two = two_of<M>(e[i][0], e[i][1]);
                 ph[i >> 1][n][i & 1] = transposed(two);
-                if constexpr (kPair) {                        // what the rounding has left
-                    const M* const held = reinterpret_cast<const M*>(&two);
-                    pl[i >> 1][n][i & 1] = transposed(two_of<M>(e[i][0] - widen_at(held, 0), e[i][1] - widen_at(held, 1)));
-                }
+                const M* const held = reinterpret_cast<const M*>(&two);                  // and what the rounding has left
+                pl[i >> 1][n][i & 1] = transposed(two_of<M>(e[i][0] - widen_at(held, 0), e[i][1] - widen_at(held, 1)));
             }
         }
         if (__any_sync(0xffffffffu, moved)) {
@@ -525,7 +523,7 @@ struct MmaWarp {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     mma(acc[s][n], a, ph[b][n][0], ph[b][n][1], M());
-                    if constexpr (kPair) mma(acc[s][n], a, pl[b][n][0], pl[b][n][1], M());
+                    mma(acc[s][n], a, pl[b][n][0], pl[b][n][1], M());
                 }
             };
             if constexpr (kCodes) {
@@ -579,13 +577,13 @@ struct MmaWarp {
                 for (int i = 0; i < 2 * kSub; ++i) {          // (masks: an index that the loop works out would put the arrays into local memory)
                     const uint32_t its = i == at >> 3 ? 0xffffffffu : 0u;
                     high |= ph[i >> 1][n][i & 1] & its;
-                    if constexpr (kPair) low |= pl[i >> 1][n][i & 1] & its;
+                    low |= pl[i >> 1][n][i & 1] & its;
                 }
                 high = __shfl_sync(0xffffffffu, transposed(high), from);
-                if constexpr (kPair) low = __shfl_sync(0xffffffffu, transposed(low), from);
+                low = __shfl_sync(0xffffffffu, transposed(low), from);
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    p[n][j] = widen_at(reinterpret_cast<const M*>(&high), j) + (kPair ? widen_at(reinterpret_cast<const M*>(&low), j) : 0.0f);
+                    p[n][j] = widen_at(reinterpret_cast<const M*>(&high), j) + widen_at(reinterpret_cast<const M*>(&low), j);
             }
 #pragma unroll
             for (int s = 0; s < DH / 16; ++s) {

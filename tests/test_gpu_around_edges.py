@@ -259,3 +259,30 @@ def test_logits_of_minus_infinity_on_codes(ctx, dt, lens, hq, dh):
         paged.v[page, place] = 0x7F
     got, lse = attend_to(ctx, paged, Q, lens, dt)
     assert (got[:, 0::2] == 0).all() and got[:, 1::2].isnan().all()
+
+
+# ---- precision of the weights ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt,cache", [("bf16", "e4m3"), ("f16", "e4m3"), ("bf16", "bf16"), ("f16", "f16")])
+@pytest.mark.parametrize("n,hq", [(2, 1), (40, 1), (400, 12)])
+def test_weights_of_more_than_half_precision(ctx, dt, cache, n, hq):
+    """Two kinds of keys whose values all but cancel: the weight of one kind lies next to 7/8, so close that eleven bits of it would leave a zero."""
+    dh = 64
+    to_store = (lambda x: x.to(torch.float8_e4m3fn).view(torch.uint8)) if cache == "e4m3" else (lambda x: x.to(DT[cache]))
+    k, v = torch.zeros((n, 1, 1, dh), device="cuda"), torch.full((n, 1, 1, dh), 0.875, device="cuda")
+    k[1::2, 0, 0, 0], v[1::2] = -1.0, -1.0
+    table = torch.arange(n, dtype=torch.int32, device="cuda")[None]
+    paged = binding.PagedCache(to_store(k), to_store(v), table)
+    Q = torch.zeros((1, hq * dh), dtype=DT[dt], device="cuda")
+    Q[:, ::dh] = 1.0
+    off = 0.9 * 2.0 ** -12 if cache != "bf16" else 0.9 * 2.0 ** -10
+    scale = -math.log(0.875 * (1 + off))
+    scale = torch.tensor(scale, dtype=torch.float32).item()
+    ln, o, lse = torch.tensor([n], dtype=torch.int32, device="cuda"), torch.empty_like(Q), torch.empty((1, hq), device="cuda")
+    ctx.paged_attention(paged, Q, ln, o, scale=scale, lse=lse)
+    o64, l64, weight, slack = ref.attend(Q.reshape(1, hq, dh), paged.k, paged.v, table, [n], scale)
+    # the stored result's rounding; the logit and exp as in attend_tolerance, a pair of 16-bit values for each weight, sums of n terms
+    rel = 2 * slack[..., None] + 2.0 ** -21 * (1 + l64.abs())[..., None] + (n + 16) * 2.0 ** -24 + (2.0 ** -16 if cache == "bf16" else 2.0 ** -21)
+    tol = ref.HALF_STEP[dt] * o64.abs() + rel * weight + 2.0 ** -25
+    assert (o64.abs() > 2 * tol).all()                          # a zero would be seen
+    assert ((o.reshape(1, hq, dh).double() - o64).abs() <= tol).all()
