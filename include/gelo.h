@@ -366,12 +366,12 @@ int gelo_qkv_offload_blockdiag_batch(gelo_ctx* ctx, int calls, const void* const
 
 /* Root-mean-square norm of `rows` rows of d values, with the residual's addition:
  *     h = X + R (R_dev may be NULL: h = X),  y = h / sqrt(mean(h^2) + eps) * weight  (weight_dev, d values, may be NULL: 1).
- *   R_out_dev (optional, only with R_dev; may be R_dev or X_dev itself) receives h.
- *   Y_dev (optional; may be X_dev itself) receives y in `dtype`.
+ *   R_out_dev (optional, only with R_dev; may be R_dev or X_dev itself with the same stride) receives h.
+ *   Y_dev (optional; may be X_dev or R_dev itself with the same stride, if R_out_dev is not) receives y in `dtype`.
  *   codes_dev (optional) receives E4M3 codes and row_scale_dev (rows floats) their scales: scale = max|y_row| / 448 (1 for a
  *     row of zeros), code = nearest-even E4M3 of y / scale (y not rounded to `dtype` in between), saturating; with it d has to
  *     be a multiple of 16.  A row that holds a NaN or an infinity gets a NaN scale and NaN codes.
- * At least one of Y_dev and codes_dev is given.  y is formed from the unrounded h.  8 <= d <= 65536, a multiple of 8.  A row of magnitudes over
+ * At least one of Y_dev and codes_dev is given; otherwise results overlap neither the inputs nor one another.  y is formed from the unrounded h.  8 <= d <= 65536, a multiple of 8.  A row of magnitudes over
  * 1e16 overflows the fp32 sum of squares and counts as infinite.  rows = 0 is a no-op. */
 int gelo_rms_norm(gelo_ctx* ctx, const void* X_dev, int ldx, const void* R_dev, int ldr, const void* weight_dev, int rows, int d,
                   float eps, int dtype, void* R_out_dev, int ldro, void* Y_dev, int ldy, void* codes_dev, int ldc,

@@ -1401,6 +1401,13 @@ int gelo_rms_norm(gelo_ctx* ctx, const void* X_dev, int ldx, const void* R_dev, 
         (reinterpret_cast<uintptr_t>(row_scale_dev) & 3u) || bad_row_stride(ldx, d, 8) || (R_dev && bad_row_stride(ldr, d, 8)) ||
         (R_out_dev && bad_row_stride(ldro, d, 8)) || (Y_dev && bad_row_stride(ldy, d, 8)))
         return GELO_ERR_INVALID;
+    // A result may take the place of an input row by row only: with another stride one row's stores would meet rows that others have yet to read.
+    auto displaces = [rows](const void* out, int ldo, const void* in, int ldi) { return out && out == in && rows > 1 && ldo != ldi; };
+    if (displaces(Y_dev, ldy, X_dev, ldx) || displaces(Y_dev, ldy, R_dev, ldr) || displaces(R_out_dev, ldro, X_dev, ldx) || displaces(R_out_dev, ldro, R_dev, ldr))
+        return GELO_ERR_INVALID;
+    if ((Y_dev && (Y_dev == R_out_dev || Y_dev == weight_dev)) || (R_out_dev && R_out_dev == weight_dev)) return GELO_ERR_INVALID;
+    for (const void* other : { X_dev, R_dev, weight_dev, (const void*)R_out_dev, (const void*)Y_dev })
+        if (codes_dev && codes_dev == other) return GELO_ERR_INVALID;
     DeviceGuard guard(ctx->device);
     return launch_rms_norm(ctx, X_dev, ldx, R_dev, ldr, weight_dev, rows, d, eps, dtype, R_out_dev, ldro, Y_dev, ldy, codes_dev, ldc, row_scale_dev,
                            as_stream(stream));

@@ -28,3 +28,16 @@ def test_attention_workspace(lib, ctx):
     assert lib.gelo_set_attention_workspace(ctx, P, need - 1) == WORKSPACE
     assert lib.gelo_set_attention_workspace(ctx, P, need) == OK
     assert lib.gelo_set_attention_workspace(ctx, None, 0) == OK
+
+
+def test_norm_in_place_keeps_the_stride(lib, ctx):
+    """One row's results must not land on rows that others have yet to read."""
+    A, B, C = P, 2 * P, 3 * P
+
+    def norm(x=A, ldx=64, r=None, ldr=0, w=None, rows=3, d=64, ro=None, ldro=0, y=B, ldy=64, c=None, ldc=0, s=None):
+        return lib.gelo_rms_norm(ctx, x, ldx, r, ldr, w, rows, d, 1e-5, binding.BF16, ro, ldro, y, ldy, c, ldc, s, None)
+
+    for bad in (dict(y=A, ldy=128), dict(y=A, ldx=128), dict(r=B, ldr=128), dict(r=C, ldr=64, ro=C, ldro=72), dict(r=C, ldr=64, ro=A, ldro=128), dict(r=C, ldr=64, ro=B, ldro=64),
+                dict(r=C, ldr=64, y=A, ro=A, ldro=64), dict(w=B), dict(r=C, ldr=64, w=C, ro=C, ldro=64), dict(c=A, ldc=64, s=P), dict(c=B, ldc=64, s=P),
+                dict(c=C, ldc=64, s=P, r=C, ldr=64), dict(c=C, ldc=64, s=P, w=C), dict(rows=1, r=C, ldr=64, ro=B, ldro=64)):
+        assert norm(**bad) == INVALID, bad

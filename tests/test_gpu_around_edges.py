@@ -286,3 +286,27 @@ def test_weights_of_more_than_half_precision(ctx, dt, cache, n, hq):
     tol = ref.HALF_STEP[dt] * o64.abs() + rel * weight + 2.0 ** -25
     assert (o64.abs() > 2 * tol).all()                          # a zero would be seen
     assert ((o.reshape(1, hq, dh).double() - o64).abs() <= tol).all()
+
+
+# ---- norm ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d", [512, 4096, 20000])
+def test_norm_in_the_place_of_either_input(ctx, d):
+    x, r, w = rnd(90, 9, d, dtype="bf16"), rnd(91, 9, d, dtype="bf16"), rnd(92, d, dtype="bf16")
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    ctx.rms_norm(x, y, weight=w, residual=r, residual_out=h)
+    for out, out_h in ((0, 1), (1, 0), (1, None), (0, None), (None, 0), (None, 1)):
+        xs, rs = x.clone(), r.clone()
+        spare = torch.empty_like(x)
+        ys = spare if out is None else (xs, rs)[out]
+        hs = None if out_h is None else (xs, rs)[out_h]
+        ctx.rms_norm(xs, ys, weight=w, residual=rs, residual_out=hs)
+        assert torch.equal(ys, y) and (hs is None or torch.equal(hs, h))
+    wide = torch.empty((18, d), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(binding.GeloError) as e:
+        ctx.rms_norm(wide[::2], wide[:9], weight=w)
+    assert e.value.status == binding.ERR_INVALID
+    one = wide[:1]
+    one.copy_(x[:1])
+    ctx.rms_norm(one, one, weight=w, residual=r[:1])
+    assert torch.equal(one, y[:1])
