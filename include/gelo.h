@@ -379,8 +379,9 @@ int gelo_rms_norm(gelo_ctx* ctx, const void* X_dev, int ldx, const void* R_dev, 
 
 /* Rotary positions.  Pair i of the first `rot` components of a head turns by turns[i] of a full circle per position:
  *     x_a' = (x_a cos - x_b sin) * magnitude,  x_b' = (x_b cos + x_a sin) * magnitude,   angle = 2 pi position turns[i],
- * (a, b) = (i, i + rot / 2), or (2i, 2i + 1) if `interleaved`.  Components from `rot` on stay as they are.  The angle is reduced to one
- * circle in binary64, so positions up to 2^31 - 1 keep fp32 accuracy.
+ * (a, b) = (i, i + rot / 2), or (2i, 2i + 1) if `interleaved`.  Components from `rot` on stay as they are.  position * turns[i]
+ * is reduced to one circle exactly, so that positions up to 2^31 - 1 keep fp32 accuracy with respect to the turns given.  Those of gelo_rope_turns
+ * are good to 2^-50 relative where nothing is stretched, which is up to position * 2^-50 radians: less than fp32's 2^-24 up to position 2^26.
  * gelo_rope_turns fills turns_dev (rot / 2 doubles, 8-byte aligned) with t = base^(-2i / rot) / (2 pi), for long contexts stretched:
  *     t' = t (g + (1 - g) / factor),  g = clamp((original * t - low) / (high - low), 0, 1),
  * i.e. pairs that turn at least `high` times within the original context stay, those that turn at most `low` times are interpolated by

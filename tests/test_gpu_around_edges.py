@@ -1,5 +1,7 @@
 """Orders, captures and values at the edges of what the calls around the projection allow."""
 import math
+from decimal import Decimal, localcontext
+from fractions import Fraction
 
 import pytest
 import torch
@@ -310,3 +312,57 @@ def test_norm_in_the_place_of_either_input(ctx, d):
     one.copy_(x[:1])
     ctx.rms_norm(one, one, weight=w, residual=r[:1])
     assert torch.equal(one, y[:1])
+
+
+# ---- rotation ------------------------------------------------------------------------------------------
+
+FAR = [0, 1, 8191, 131071, 1 << 24, (1 << 26) - 1, (1 << 30) + 12345, 2 ** 31 - 1]
+
+
+def unit_pairs(heads, dh, rot, inter):
+    """Heads whose pairs are (1, 0), so that a rotation writes cosines and sines; where they stand."""
+    x = torch.zeros((len(FAR), heads, dh), device="cuda")
+    i = torch.arange(rot // 2, device="cuda")
+    a, b = (2 * i, 2 * i + 1) if inter else (i, i + rot // 2)
+    x[:, :, a] = 1.0
+    return x.reshape(len(FAR), -1), a, b
+
+
+def circle(parts):
+    """Cosines and sines of exact fractions of a circle."""
+    angle = torch.tensor([[2 * math.pi * float(t - round(t)) for t in row] for row in parts], dtype=torch.float64, device="cuda")
+    return angle.cos(), angle.sin()
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dh,rot", [(128, 128), (64, 20)])
+def test_rotation_is_exact_about_the_turns_it_is_given(ctx, dh, rot, inter):
+    """Each cosine and sine is that of the exact product of position and turns, rounded once (and the angle to binary64, 2^-50 radians)."""
+    turns = torch.empty(rot // 2, dtype=torch.float64, device="cuda")
+    ctx.rope_turns(turns)
+    x, a, b = unit_pairs(2, dh, rot, inter)
+    y = torch.empty_like(x)
+    ctx.rotary(x, 2, torch.tensor(FAR, dtype=torch.int32, device="cuda"), binding.Rope(turns, interleaved=inter), y)
+    c, s = circle([[pos * Fraction(t) for t in turns.tolist()] for pos in FAR])
+    y = y.reshape(len(FAR), 2, dh).double()
+    for want, at in ((c, a), (s, b)):
+        assert ((y[:, :, at] - want[:, None]).abs() <= 2.0 ** -24 * want.abs()[:, None] + 2.0 ** -50).all()
+
+
+@pytest.mark.parametrize("base", [10000.0, 500000.0])
+def test_rotation_of_far_positions(ctx, base):
+    """The whole angle against one worked out with 60 digits: the stored rounding, and what the turns' own costs."""
+    rot = 128
+    turns = torch.empty(rot // 2, dtype=torch.float64, device="cuda")
+    ctx.rope_turns(turns, base=base)
+    with localcontext() as digits:
+        digits.prec = 60
+        pi = Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+        exact = [Fraction((Decimal(base).ln() * (-2 * i) / rot).exp() / (2 * pi)) for i in range(rot // 2)]
+    x, a, b = unit_pairs(1, rot, rot, False)
+    y = torch.empty_like(x)
+    pos = torch.tensor(FAR, dtype=torch.int32, device="cuda")
+    ctx.rotary(x, 1, pos, binding.Rope(turns), y)
+    c, s = circle([[p * t for t in exact] for p in FAR])
+    for want, at in ((c, a), (s, b)):
+        assert ((y[:, at].double() - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -50 * (1 + pos.double())[:, None]).all()
