@@ -118,6 +118,16 @@ float number(PyObject* o)
 }
 gelo_ctx* context(PyObject* o) { return static_cast<gelo_ctx*>(address(o)); }
 
+// Python's lock is let go of while the library launches, as ctypes does: a launch that waits for a full queue would hold up all threads, for good if what
+// the queue waits for needs one of them.  Nothing of Python may be touched meanwhile; the caller's arguments keep the tensors alive.
+class Unlocked {
+    PyThreadState* const state = PyEval_SaveThread();
+public:
+    Unlocked() = default;
+    Unlocked(const Unlocked&) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 template <typename F>
 PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F&& call)
 {
@@ -158,8 +168,11 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
             C = rows_of(a[8], "codes", t == at::kFloat8_e4m3fn ? t : at::kByte, rows, d, device);
         }
         float* const s = values_of<float>(a[9], "row_scale", at::kFloat, rows, device, true);
-        return gelo_rms_norm(context(a[0]), X.at, X.ld, R.at, R.ld, w, (int)rows, (int)d, number(a[5]), code, O.at, O.ld, Y.at, Y.ld, C.at, C.ld, s,
-                             stream_of(a[10], device));
+        gelo_ctx* const ctx = context(a[0]);
+        const float eps = number(a[5]);
+        void* const stream = stream_of(a[10], device);
+        const Unlocked unlocked;
+        return gelo_rms_norm(ctx, X.at, X.ld, R.at, R.ld, w, (int)rows, (int)d, eps, code, O.at, O.ld, Y.at, Y.ld, C.at, C.ld, s, stream);
     });
 }
 
@@ -181,7 +194,10 @@ PyObject* project_e4m3_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor& sw = tensor(a[5], "w_scale");                                // one value, or the pair that the quantiser leaves
         const float* scale = values_of<float>(a[5], "w_scale", at::kFloat, sw.numel() == 2 ? 2 : 1, device);
         void* y = values_of<void>(a[9], "Yp", at::kBFloat16, (int64_t)m * p, device);
-        return gelo_project_e4m3_rows(context(a[0]), u, su, w, scale, m, d, p, y, stream_of(a[10], device));
+        gelo_ctx* const ctx = context(a[0]);
+        void* const stream = stream_of(a[10], device);
+        const Unlocked unlocked;
+        return gelo_project_e4m3_rows(ctx, u, su, w, scale, m, d, p, y, stream);
     });
 }
 
@@ -199,8 +215,11 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
         const Rows X = rows_of(a[2], "X", x.scalar_type(), rows, width, device);
         const Rows Y = a[6] == Py_None ? X : rows_of(a[6], "Y", x.scalar_type(), rows, width, device);
         const int* pos = values_of<int>(a[4], "pos", at::kInt, rows, device);
-        return gelo_rotary(context(a[0]), X.at, X.ld, (int)rows, heads, (int)(width / heads), pos, struct_at<gelo_rope>(a[5]), code, Y.at, Y.ld,
-                           stream_of(a[7], device));
+        gelo_ctx* const ctx = context(a[0]);
+        const gelo_rope* const rope = struct_at<gelo_rope>(a[5]);
+        void* const stream = stream_of(a[7], device);
+        const Unlocked unlocked;
+        return gelo_rotary(ctx, X.at, X.ld, (int)rows, heads, (int)(width / heads), pos, rope, code, Y.at, Y.ld, stream);
     });
 }
 
@@ -231,8 +250,11 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n)
         }
         const int* seq = values_of<int>(a[6], "seq", at::kInt, rows, device, true);
         const int* pos = values_of<int>(a[5], "pos", at::kInt, rows, device);
-        return gelo_append_kv(context(a[0]), cache, K.at, K.ld, V.at, V.ld, Q.at, Q.ld, heads, (int)rows, seq, pos, struct_at<gelo_rope>(a[7]), code, O.at,
-                              O.ld, stream_of(a[10], device));
+        gelo_ctx* const ctx = context(a[0]);
+        const gelo_rope* const rope = struct_at<gelo_rope>(a[7]);
+        void* const stream = stream_of(a[10], device);
+        const Unlocked unlocked;
+        return gelo_append_kv(ctx, cache, K.at, K.ld, V.at, V.ld, Q.at, Q.ld, heads, (int)rows, seq, pos, rope, code, O.at, O.ld, stream);
     });
 }
 
@@ -251,8 +273,12 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
         const Rows Q = rows_of(a[3], "Q", q.scalar_type(), rows, width, device), O = rows_of(a[5], "O", q.scalar_type(), rows, width, device);
         const int* lengths = values_of<int>(a[4], "lengths", at::kInt, rows, device);
         float* const lse = values_of<float>(a[8], "lse", at::kFloat, rows * heads, device, true);
-        return gelo_paged_attention(context(a[0]), cache, Q.at, Q.ld, heads, lengths, number(a[6]), whole(a[7]), code, O.at, O.ld, lse,
-                                    stream_of(a[9], device));
+        gelo_ctx* const ctx = context(a[0]);
+        const float scale = number(a[6]);
+        const int window = whole(a[7]);
+        void* const stream = stream_of(a[9], device);
+        const Unlocked unlocked;
+        return gelo_paged_attention(ctx, cache, Q.at, Q.ld, heads, lengths, scale, window, code, O.at, O.ld, lse, stream);
     });
 }
 
