@@ -106,17 +106,29 @@ def load_library():
     """Loads the CUDA library; raises if it has not been built (no fallback exists)."""
     global _lib, _marshal
     if _lib is None:
-        for path in (_LIB_PATH, os.path.join(_HERE, "_marshal.so")):
-            if not os.path.exists(path):
-                raise FileNotFoundError(f"{path} is missing: build it with `python -m paper_2603_05035_b200.build`")
+        if not os.path.exists(_LIB_PATH):
+            raise FileNotFoundError(f"{_LIB_PATH} is missing: build it with `python -m paper_2603_05035_b200.build`")
         lib = ctypes.CDLL(_LIB_PATH)
         for name, (res, args) in EXPORTS.items():
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args
-        from . import _marshal as m                              # (finds libgelo.so beside it, already loaded)
+        try:
+            from . import _marshal as m                          # (finds libgelo.so beside it, already loaded)
+        except ImportError as e:
+            m = _NoMarshal(e)
         _lib, _marshal = lib, m
     return _lib
+
+
+class _NoMarshal:
+    """In the place of ``_marshal.so`` where it has not been built or does not fit this torch: the calls that go through it raise."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"{name} needs _marshal.so: build it with `python -m paper_2603_05035_b200.build`") from self._why
 
 
 def dtype_code(dtype) -> int:
