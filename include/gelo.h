@@ -428,7 +428,7 @@ int gelo_append_kv(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* K_dev,
 
 /* Attention of one new token per sequence: row s of Q_dev (cache->seqs rows of q_heads x head_dim; q_heads a multiple of kv_heads, head h
  * reads key-value head h / (q_heads / kv_heads)) against positions max(0, len - window) .. len - 1 of sequence s, len = len_dev[s]
- * (window 0: all):   o = sum_j p_j v_j,  p = softmax_j(scale q . k_j).   O_dev: rows as Q_dev (may be Q_dev itself with the same stride).
+ * (window 0: all):   o = sum_j p_j v_j,  p = softmax_j(scale q . k_j), |scale * k_scale| at most 2e38.   O_dev: rows as Q_dev (may be Q_dev itself with the same stride).
  * lse_dev (optional, seqs x q_heads floats): log sum_j exp(scale q . k_j).  A length of zero or less gives o = 0 and lse = -infinity.
  * Entries of the cache outside those positions are not read, or do not count whatever they hold.  A length beyond the table is cut to it, and a page
  * outside the cache counts as absent; both record GELO_ERR_INVALID.  A key whose logit is minus infinity does not count either; an infinity

@@ -1473,6 +1473,7 @@ int gelo_paged_attention(gelo_ctx* ctx, const gelo_kv_cache* cache, const void* 
 {
     if (!ctx || bad_dtype(dtype) || window < 0 || !std::isfinite(scale)) return GELO_ERR_INVALID;
     GELO_TRY(check_cache(cache, dtype));
+    if (!std::isfinite(scale * cache->k_scale * 1.4426950f)) return GELO_ERR_INVALID;          // the factor of the kernel's logits, in base 2
     const int dh = cache->head_dim;
     if (q_heads < 1 || q_heads > INT_MAX / dh || (q_heads % cache->kv_heads) != 0 || bad_row_stride(ldq, q_heads * dh, 8) ||
         bad_row_stride(ldo, q_heads * dh, 8))

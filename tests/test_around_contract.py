@@ -41,3 +41,15 @@ def test_norm_in_place_keeps_the_stride(lib, ctx):
                 dict(r=C, ldr=64, y=A, ro=A, ldro=64), dict(w=B), dict(r=C, ldr=64, w=C, ro=C, ldro=64), dict(c=A, ldc=64, s=P), dict(c=B, ldc=64, s=P),
                 dict(c=C, ldc=64, s=P, r=C, ldr=64), dict(c=C, ldc=64, s=P, w=C), dict(rows=1, r=C, ldr=64, ro=B, ldro=64)):
         assert norm(**bad) == INVALID, bad
+
+
+def test_attention_scales_whose_product_overflows(lib, ctx):
+    def call(scale, k_scale, dtype=binding.E4M3):
+        c = binding._CacheStruct(k_dev=P, v_dev=P, table_dev=P, page_stride=16 * 4 * 128, token_stride=4 * 128, head_stride=128, dtype=dtype, pages=10, page_size=16,
+                                 kv_heads=4, head_dim=128, seqs=0, max_pages=5, table_ld=5, k_scale=k_scale, v_scale=1.0)
+        return lib.gelo_paged_attention(ctx, ctypes.addressof(c), P, 1024, 8, P, scale, 0, binding.BF16, P, 1024, None, None)
+
+    for scale, k_scale in ((1e30, 1e10), (-1e30, 1e10), (3e38, 1.0), (1.0, 3e38)):
+        assert call(scale, k_scale) == INVALID, (scale, k_scale)
+    assert call(3e38, 1.0, binding.BF16) == INVALID
+    assert call(2e38, 1.0, binding.BF16) == call(-1e20, 1e18) == call(1e30, 1e-10) == OK       # (no sequences: nothing is launched)
