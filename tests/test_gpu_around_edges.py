@@ -366,3 +366,54 @@ def test_rotation_of_far_positions(ctx, base):
     c, s = circle([[p * t for t in exact] for p in FAR])
     for want, at in ((c, a), (s, b)):
         assert ((y[:, at].double() - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -50 * (1 + pos.double())[:, None]).all()
+
+
+# ---- what the roundings leave, no more ----------------------------------------------------------------------
+
+def tight(o64, l64, weight, slack, lens, vmax, dt, cache):
+    """As attend_tolerance, with weights held as pairs on every cache: 16 bits (bf16) or 22, and on halves, kept relative to 2^-14 of the
+    largest, 2^-39 of it absolute."""
+    n = torch.as_tensor(lens, device=o64.device).clamp_min(1).double()[:, None, None]
+    exp = 2.0 ** -21 * (1 + l64.abs().nan_to_num(posinf=0, neginf=0))
+    rel = 2 * slack[..., None] + exp[..., None] + (n + 16) * 2.0 ** -24 + (2.0 ** -16 if cache == "bf16" else 2.0 ** -22)
+    return ref.HALF_STEP[dt] * o64.abs() + rel * weight + n * 2.0 ** -39 * vmax + 2.0 ** -25, slack + (n[..., 0] + 16) * 2.0 ** -24 + exp
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("lens,hq,hk,dh,window", [([21000], 1, 1, 128, 0), ([21000], 32, 1, 64, 14000), ([30001], 16, 1, 256, 0), ([9001, 20000], 3, 1, 96, 0),
+                                                  ([24000] + [5, 900, 0] * 13, 8, 2, 128, 0), ([5000], 16, 2, 128, 100), ([700] * 3, 32, 32, 128, 0),
+                                                  ([(37 * i) % 23 for i in range(700)], 2, 1, 32, 0), ([1, 0, 17, 16, 15, 333, 64, 130, -4, 2], 40, 1, 64, 20)])
+def test_attention_on_codes_to_the_last_part(ctx, dt, lens, hq, hk, dh, window):
+    """E4M3 caches within what is rounded: a missing part of a head, however small, would stand out."""
+    paged, scales = filled(dh + 1, lens, 32, hk, dh, "token", "e4m3")
+    Q = rnd(83, len(lens), hq * dh, scale=2.0, dtype=dt)
+    o, lse = torch.empty_like(Q), torch.empty((len(lens), hq), device="cuda")
+    ctx.paged_attention(paged, Q, torch.tensor(lens, dtype=torch.int32, device="cuda"), o, window=window, lse=lse)
+    want = ref.attend(Q.reshape(len(lens), hq, dh), paged.k, paged.v, paged.table, lens, dh ** -0.5, window, *scales.values())
+    tol_o, tol_l = tight(*want, lens, ref.values(paged.v).nan_to_num().abs().max() / 20, dt, "e4m3")
+    assert ((o.reshape(want[0].shape).double() - want[0]).abs() <= tol_o).all()
+    empty = torch.isinf(want[1])
+    assert (((lse.double() - want[1]).abs() <= tol_l) | empty).all() and torch.isneginf(lse[empty]).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,d", [(40, 64), (40, 512), (300, 1024), (40, 2048), (1000, 2048), (40, 4096), (1000, 4096), (400, 8192), (20, 20000)])
+def test_norm_codes_on_middles(ctx, dt, rows, d):
+    """Rows whose quotients by the largest are the middles of two codes: the rounding of the stored scale decides, the same way for all of a row.
+    The row's factor in fp32 would take the wrong side by the hundred."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    odd = 17.0 + 2 * torch.randint(0, 8, (rows, d), generator=g, device="cuda")
+    x = odd * torch.exp2(torch.randint(-6, 4, (rows, d), generator=g, device="cuda").float())
+    x = torch.where(torch.rand((rows, d), generator=g, device="cuda") < 0.5, x, -x)
+    x[:, 0] = 448.0
+    x = (x * 2.0 ** -4).to(DT[dt])
+    codes, scale = torch.empty((rows, d), dtype=torch.uint8, device="cuda"), torch.empty(rows, device="cuda")
+    ctx.rms_norm(x, None, eps=1e-5, codes=codes, row_scale=scale)
+    _, y64 = ref.norm(x, None, None, 1e-5)
+    want = ref.to_e4m3(y64 / scale.double()[:, None])
+    inv = torch.rsqrt(x.float().square().mean(1, keepdim=True) + 1e-5)
+    fp32 = ref.to_e4m3((x.float() * (inv / scale[:, None])).double())
+    assert (fp32 != want).sum() > rows * d / 100
+    # binary64 sums of exact squares and a factor of 48 bits: the side is right unless the scale's rounding is below 2^-46
+    assert ((y64 / scale.double()[:, None])[:, 0] / 448 - 1).abs().min() > 2.0 ** -46
+    assert torch.equal(ref.values(codes), want)
