@@ -243,7 +243,8 @@ int gelo_project_e4m3(gelo_ctx* ctx, const void* U8_dev, const float* u_scale_de
                       int m, int d, int p, void* Yp_dev, void* stream);
 
 /* The same with one scale per ROW of U: Yp_dev[i] = (u_scale_dev[i] * w_scale_dev[0]) * (U8[i] * W8), u_scale_dev m floats.
- * Takes the rows that gelo_rms_norm left as codes. */
+ * Takes the rows that gelo_rms_norm left as codes, as they are: the product of a layer that is not obfuscated, since the rows of a norm have not been
+ * mixed (mixed rows become codes by gelo_quantize_e4m3, with one scale for all). */
 int gelo_project_e4m3_rows(gelo_ctx* ctx, const void* U8_dev, const float* u_scale_dev, const void* W8_dev, const float* w_scale_dev,
                            int m, int d, int p, void* Yp_dev, void* stream);
 
@@ -370,7 +371,8 @@ int gelo_qkv_offload_blockdiag_batch(gelo_ctx* ctx, int calls, const void* const
  *   Y_dev (optional; may be X_dev or R_dev itself with the same stride, if R_out_dev is not) receives y in `dtype`.
  *   codes_dev (optional) receives E4M3 codes and row_scale_dev (rows floats) their scales: scale = max|y_row| / 448 (1 for a
  *     row of zeros), code = nearest-even E4M3 of y / scale (y not rounded to `dtype` in between), saturating; with it d has to
- *     be a multiple of 16.  A row that holds a NaN or an infinity gets a NaN scale and NaN codes.
+ *     be a multiple of 16.  A row that holds a NaN or an infinity gets a NaN scale and NaN codes.  (Rows whose
+ *     largest |h weight| lies below 2e-36 lose codes to fp32's range.)
  * At least one of Y_dev and codes_dev is given; otherwise results overlap neither the inputs nor one another.  y is formed from the unrounded h.  8 <= d <= 65536, a multiple of 8.  A row of magnitudes over
  * 1e16 overflows the fp32 sum of squares and counts as infinite.  rows = 0 is a no-op. */
 int gelo_rms_norm(gelo_ctx* ctx, const void* X_dev, int ldx, const void* R_dev, int ldr, const void* weight_dev, int rows, int d,

@@ -390,7 +390,7 @@ class Context:
                                                 _stream(stream)), "gelo_project_e4m3")
 
     def project_e4m3_rows(self, U8, u_scale, W8, w_scale, m, d, p, Yp, stream=None):
-        """Yp (bf16) = u_scale[:, None] * w_scale * (U8 @ W8) on E4M3 operands: a scale per row of U8 (as rms_norm leaves them)."""
+        """Yp (bf16) = u_scale[:, None] * w_scale * (U8 @ W8) on E4M3 operands: a scale per row of U8 (as rms_norm leaves them, not obfuscated)."""
         self._check(_marshal.project_e4m3_rows(self._handle, self.device, U8, u_scale, W8, w_scale, m, d, p, Yp, stream),
                     "gelo_project_e4m3_rows")
 
@@ -440,7 +440,8 @@ class Context:
 
     def paged_attention(self, cache, Q, lengths, O, scale=None, window=0, lse=None, stream=None):
         """O = attention of one new token per sequence (row s of Q: q_heads heads) over the first lengths[s] positions of the cache, or the last
-        `window` of them; scale defaults to head_dim^-1/2; lse (sequences x q_heads, fp32) receives the logarithm of the softmax's sum."""
+        `window` of them; scale defaults to head_dim^-1/2; lse (sequences x q_heads, fp32) receives the logarithm of the softmax's sum.
+        Works in the scratch of ensure_attention_workspace, which a captured call needs; else in the general workspace."""
         self._here(cache)
         self._check(_marshal.paged_attention(self._handle, self.device, cache.ref, Q, lengths, O, cache.default_scale if scale is None else scale,
                                              window, lse, stream), "gelo_paged_attention")

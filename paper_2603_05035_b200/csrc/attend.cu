@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a paged key-value cache.
 //   o = sum_j p_j v_j,  p_j = exp(s_j - m) / l,  s_j = scale q . k_j,  m = max_j s_j,  l = sum_j exp(s_j - m)
 // One pass over the keys and values with the running maximum and sum of the softmax; every key and value is read once for all query
-// heads that share it (up to 16; more heads read them again, from L2).  Bound by HBM: 4 heads-per-group flops per element read.
+// heads that share it (up to 16, on fp32 caches 8, or 4 with heads over 128; more heads read them again, from L2).  Bound by HBM: 4 heads-per-group flops per element read.
 //
 // The work of a call is one line of tiles: sequence after sequence, key-value head after head, 16 or 32 positions a tile.  Every CTA works out
 // from the lengths which equal share of that line is its own, so ragged lengths balance and one long sequence fills the GPU.  What of
@@ -11,9 +11,9 @@
 // Inside a CTA the warps take the tiles of a segment in turn, each with a ring of its own in shared memory that asynchronous 16-byte copies
 // fill, so nothing but a segment's end makes them wait for one another.
 //
-// Measured (keys and values over time, against a copy's 6509 GB/s): 64 sequences of 100 to 4096, 32 heads of 128, bf16 310 to 324 us (97 to 101%);
-// the same in fp32 597 us (105%, reads alone run faster than a copy), E4M3 196 us (80%, bound by the widening of the codes); one sequence of 32768
-// bf16 86 us (96%); 8 of 32 heads on E4M3 111 us (90%).  Two CTAs of four warps per SM: with one of eight the end of a segment leaves the SM
+// Measured (keys and values over time, against a copy's 6509 GB/s): 64 sequences of 100 to 4096, 32 heads of 128, bf16 314 to 327 us (96 to 100%);
+// the same in fp32 597 to 621 us (101 to 105%, reads alone run faster than a copy), E4M3 188 to 197 us (80 to 84%, bound by the widening of the codes); one sequence of 32768
+// bf16 86 us (96%); 8 of 32 heads on E4M3 108 us (93%).  Two CTAs of four warps per SM: with one of eight the end of a segment leaves the SM
 // idle (64 sequences 364 us against 345 at the time).
 #include <float.h>
 #include <limits.h>
@@ -306,7 +306,8 @@ struct Joint {
 // can feed (24 instructions per 8 KB tile of 128 components).  p is handed to the second product as the 16-bit value and what
 // that leaves out, i.e. with 16 bits (bf16 caches) or 22, so that the stored result is rounded once.  (E4M3 caches with bf16 results, p as one half of 11 bits: half
 // the second products; 33 long sequences, 8 of 32 heads 108 us as with both, 16 heads a key-value head 141 instead of 156; 5 times the distance from a form in fp32.)
-// E4M3 tiles are widened to half in registers, q is given the same type times a power of two that puts its largest component into [1, 2).
+// E4M3 tiles are widened to half in registers, q is given the same type times a power of two that puts its largest component into [1, 2): components below 2^-14 of that (of
+// bf16, 2^-17) are held to 2^-25 of it, which is what fp32 sums of the products keep.
 template <typename T, bool kCodes, int DH, int NT>
 struct MmaWarp {
     using M = std::conditional_t<kCodes, __half, T>;

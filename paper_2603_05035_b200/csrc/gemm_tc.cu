@@ -1481,7 +1481,8 @@ int launch_gemm_e4m3(gelo_ctx* ctx, int M, int N, int K, const void* A8, int lda
     EncodeTiledFn enc = reinterpret_cast<EncodeTiledFn>(ctx->tmap_encode);
     // Narrow tiles while they still find an SM each: W is then streamed by twice as many SMs (K = 4096, N = 12288: 64 rows 18.3 -> 15.0 us; 1075 rows,
     // N = 1424 17.3 -> 15.3), unless so many SMs ask for the same few lines of A that they wait for one another (8 rows, N = 12288: 18.1
-    // with wide tiles, 20.9 with narrow ones; N = 8192: 17.2, 15.6).
+    // with wide tiles, 20.9 with narrow ones; N = 8192: 17.2, 15.6).  K of 256 to 8192, N of 1536 to 16384, 1 to 1075 rows: nowhere slower than wide tiles
+    // (what it leaves: 16 or 24 rows of K = 8192, N = 12288 30.0, narrow 23.8; 1 and 8 rows 31, 36 to 38).
     const int narrow_tiles = ceil_div(M, BM) * ceil_div(N, 128);
     const bool narrow = narrow_tiles <= ctx->sm_count && (M >= 32 || narrow_tiles <= 72);
     const bool pair = !narrow && use_pair(ctx, M, N, 1, false, TC_STORE_BF16);

@@ -2,7 +2,7 @@
 //   h = x + r,  y = h (mean h^2 + eps)^-1/2 w,  scale = max|y| / 448,  code = E4M3(y / scale)
 // The maximum of |y| is that of |h w| times the row's factor, so one pass over the row collects the sum of squares and the maximum, with
 // the row in registers; the second half writes from there.  Bound by HBM: x and r in, h and y out.  4096 x 4096 bf16, 134 MB: 22.8 us, 90% of a copy's rate
-// (8192 wide 43 us, 95%); 1075 rows to E4M3 7.3 us (65%: what decides a code on the right side of a middle takes the rest); 64 rows 2.7 us.
+// (8192 wide 43 us, 95%); 1075 rows to E4M3 7.3 us (65%: one wave of CTAs, which load and then convert, and what decides a code on the right side of a middle); 64 rows 2.7 us.
 #include <float.h>
 
 #include "common.cuh"
@@ -223,6 +223,7 @@ int launch_typed(gelo_ctx* ctx, const NormArgs& p, cudaStream_t st)
     // a wave of wide ones (five CTAs of 256 threads per SM, two of 512): 1000 rows of 2048 4.8 us against 5.3 with the wide shape, of 8192 16.5 against 18.5, 4096 rows 51.6
     // against 60; few rows the other way, 148 of 2048 3.3 against 2.8, of 8192 4.8 against 4.1.  The thin shape of 4096 needs so many registers that
     // it gains only where its wave of 8 per SM takes all: 1075 rows 7.3 against 8.0, 1480 rows 13.0 against 10.6, 4096 rows 28.3 against 27.5.
+    // With the residual stored too, thin and wide: 1075 rows of 2304 6.9, 8.3, of 3584 9.1, 9.7, of 4096 10.1, 10.2 (740 rows 9.1, 7.0; 1500 14.1, 12.9).
     const int groups = p.d / 8, per_sm = ceil_div(p.rows, ctx->sm_count);
     if (groups <= 32) return launch_as<T, 32, 1, kCodes>(ctx, p, st);
     if (groups <= 64) return launch_as<T, 32, 2, kCodes>(ctx, p, st);
