@@ -5,6 +5,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cxxabi.h>
 #include <limits.h>
 #include <stdio.h>
 
@@ -119,14 +120,16 @@ float number(PyObject* o)
 gelo_ctx* context(PyObject* o) { return static_cast<gelo_ctx*>(address(o)); }
 
 // Python's lock is let go of while the library launches, as ctypes does: a launch that waits for a full queue would hold up all threads, for good if what
-// the queue waits for needs one of them.  Nothing of Python may be touched meanwhile; the caller's arguments keep the tensors alive.
-class Unlocked {
+// the queue waits for needs one of them.  Nothing of Python may be touched meanwhile; the caller's arguments keep the tensors alive.  (No destructor takes the
+// lock back: where the interpreter is ending, that unwinds the thread.)
+template <typename F>
+int unlocked(F&& call)
+{
     PyThreadState* const state = PyEval_SaveThread();
-public:
-    Unlocked() = default;
-    Unlocked(const Unlocked&) = delete;
-    ~Unlocked() { PyEval_RestoreThread(state); }
-};
+    const int status = call();                                // (throws nothing)
+    PyEval_RestoreThread(state);
+    return status;
+}
 
 template <typename F>
 PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F&& call)
@@ -142,6 +145,8 @@ PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F&& call)
         PyErr_SetString(PyExc_ValueError, r.text);
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (const abi::__forced_unwind&) {
+        throw;                                                // the thread is ending (see unlocked)
     } catch (...) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "unknown error");
     }
@@ -171,8 +176,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
         gelo_ctx* const ctx = context(a[0]);
         const float eps = number(a[5]);
         void* const stream = stream_of(a[10], device);
-        const Unlocked unlocked;
-        return gelo_rms_norm(ctx, X.at, X.ld, R.at, R.ld, w, (int)rows, (int)d, eps, code, O.at, O.ld, Y.at, Y.ld, C.at, C.ld, s, stream);
+        return unlocked([&] { return gelo_rms_norm(ctx, X.at, X.ld, R.at, R.ld, w, (int)rows, (int)d, eps, code, O.at, O.ld, Y.at, Y.ld, C.at, C.ld, s, stream); });
     });
 }
 
@@ -196,8 +200,7 @@ PyObject* project_e4m3_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
         void* y = values_of<void>(a[9], "Yp", at::kBFloat16, (int64_t)m * p, device);
         gelo_ctx* const ctx = context(a[0]);
         void* const stream = stream_of(a[10], device);
-        const Unlocked unlocked;
-        return gelo_project_e4m3_rows(ctx, u, su, w, scale, m, d, p, y, stream);
+        return unlocked([&] { return gelo_project_e4m3_rows(ctx, u, su, w, scale, m, d, p, y, stream); });
     });
 }
 
@@ -218,8 +221,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n)
         gelo_ctx* const ctx = context(a[0]);
         const gelo_rope* const rope = struct_at<gelo_rope>(a[5]);
         void* const stream = stream_of(a[7], device);
-        const Unlocked unlocked;
-        return gelo_rotary(ctx, X.at, X.ld, (int)rows, heads, (int)(width / heads), pos, rope, code, Y.at, Y.ld, stream);
+        return unlocked([&] { return gelo_rotary(ctx, X.at, X.ld, (int)rows, heads, (int)(width / heads), pos, rope, code, Y.at, Y.ld, stream); });
     });
 }
 
@@ -253,8 +255,7 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n)
         gelo_ctx* const ctx = context(a[0]);
         const gelo_rope* const rope = struct_at<gelo_rope>(a[7]);
         void* const stream = stream_of(a[10], device);
-        const Unlocked unlocked;
-        return gelo_append_kv(ctx, cache, K.at, K.ld, V.at, V.ld, Q.at, Q.ld, heads, (int)rows, seq, pos, rope, code, O.at, O.ld, stream);
+        return unlocked([&] { return gelo_append_kv(ctx, cache, K.at, K.ld, V.at, V.ld, Q.at, Q.ld, heads, (int)rows, seq, pos, rope, code, O.at, O.ld, stream); });
     });
 }
 
@@ -277,8 +278,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
         const float scale = number(a[6]);
         const int window = whole(a[7]);
         void* const stream = stream_of(a[9], device);
-        const Unlocked unlocked;
-        return gelo_paged_attention(ctx, cache, Q.at, Q.ld, heads, lengths, scale, window, code, O.at, O.ld, lse, stream);
+        return unlocked([&] { return gelo_paged_attention(ctx, cache, Q.at, Q.ld, heads, lengths, scale, window, code, O.at, O.ld, lse, stream); });
     });
 }
 

@@ -1,5 +1,6 @@
 """Orders, captures and values at the edges of what the calls around the projection allow."""
 import math
+import threading
 from decimal import Decimal, localcontext
 from fractions import Fraction
 
@@ -181,7 +182,7 @@ LENS = [[40, 5000, 17, 1], [(37 * i) % 23 + 1 for i in range(700)], [33] * 40]
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("lens", LENS, ids=["cut", "alone", "whole"])
-@pytest.mark.parametrize("hq,hk,dh", [(1, 1, 64), (8, 2, 128), (14, 1, 64), (12, 1, 256), (3, 1, 80)])
+@pytest.mark.parametrize("hq,hk,dh", [(1, 1, 64), (8, 2, 128), (14, 1, 64), (11, 1, 256), (3, 1, 80)])
 def test_values_behind_keys_of_minus_infinity(ctx, dt, lens, hq, hk, dh):
     """Keys of minus infinity, whole tiles of them too: their values do not count, be they infinite or NaN."""
     ps = 8
@@ -208,7 +209,7 @@ def test_values_behind_keys_of_minus_infinity(ctx, dt, lens, hq, hk, dh):
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("lens", LENS, ids=["cut", "alone", "whole"])
-@pytest.mark.parametrize("hq,dh", [(4, 64), (8, 128), (14, 64), (12, 256)])
+@pytest.mark.parametrize("hq,dh", [(4, 64), (8, 128), (14, 64), (11, 256)])
 def test_keys_of_minus_infinity_for_some_heads(ctx, dt, lens, hq, dh):
     """Keys so large that the logits of every other head overflow: those heads pass over the value, the others do not, and see an infinity in it."""
     ps = 16
@@ -243,7 +244,7 @@ def test_keys_of_minus_infinity_for_some_heads(ctx, dt, lens, hq, dh):
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 @pytest.mark.parametrize("lens", LENS, ids=["cut", "alone", "whole"])
-@pytest.mark.parametrize("hq,dh", [(2, 64), (8, 128), (14, 64), (12, 256)])
+@pytest.mark.parametrize("hq,dh", [(2, 64), (8, 128), (14, 64), (11, 256)])
 def test_logits_of_minus_infinity_on_codes(ctx, dt, lens, hq, dh):
     """A query of minus infinity makes every logit of its head one: that head is zero whatever the values hold, and sees none of its neighbours'."""
     ps = 16
@@ -417,3 +418,55 @@ def test_norm_codes_on_middles(ctx, dt, rows, d):
     # binary64 sums of exact squares and a factor of 48 bits: the side is right unless the scale's rounding is below 2^-46
     assert ((y64 / scale.double()[:, None])[:, 0] / 448 - 1).abs().min() > 2.0 ** -46
     assert torch.equal(ref.values(codes), want)
+
+
+# ---- threads --------------------------------------------------------------------------------------------
+
+def test_threads_with_contexts_of_their_own():
+    """Three threads, each with a context and a stream, make the calls of a step at once; the results are those of the calls one by one."""
+    def step(c, set_, out, stream):
+        x, w, paged, pos, ln, rope = set_
+        n, hk, dh = x.shape[0], paged.kv_heads, paged.head_dim
+        h, q, o = out
+        c.rms_norm(x, h, weight=w, stream=stream)
+        c.append_kv(paged, h[:, -2 * hk * dh:-hk * dh], h[:, -hk * dh:], pos, rope=rope, Q=h[:, :4 * hk * dh], Q_out=q, stream=stream)
+        c.paged_attention(paged, q, ln, o, stream=stream)
+
+    ctxs, sets, want = [], [], []
+    for i, hk in enumerate((1, 2, 4)):
+        c = binding.Context(0)
+        c.ensure_attention_workspace()
+        lens = [2000 + 300 * i, 9, 700]
+        paged, _ = filled(94 + i, lens, 16, hk, 64, "token", "bf16")
+        turns = torch.empty(32, dtype=torch.float64, device="cuda")
+        c.rope_turns(turns)
+        d = 6 * hk * 64
+        sets.append((rnd(95 + i, 3, d, dtype="bf16"), rnd(98 + i, d, dtype="bf16"), paged, torch.tensor(lens, dtype=torch.int32, device="cuda") - 1,
+                     torch.tensor(lens, dtype=torch.int32, device="cuda"), binding.Rope(turns)))
+        ctxs.append(c)
+    outs = [[tuple(torch.empty((3, w), dtype=torch.bfloat16, device="cuda") for w in (s[0].shape[1], 4 * s[2].kv_heads * 64, 4 * s[2].kv_heads * 64))
+             for _ in range(60)] for s in sets]
+    for c, s, o in zip(ctxs, sets, outs):
+        step(c, s, o[0], None)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in o[0]])
+    streams, failed = [torch.cuda.Stream() for _ in ctxs], []
+
+    def run(i):
+        try:
+            for o in outs[i]:
+                step(ctxs[i], sets[i], o, streams[i])
+        except Exception as e:                                   # (reported by the test's own thread)
+            failed.append(e)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(ctxs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for c, out, w in zip(ctxs, outs, want):
+        assert all(torch.equal(a, b) for o in out for a, b in zip(o, w))
+        assert c.last_status() == binding.OK
+        c.close()
